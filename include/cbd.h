@@ -386,6 +386,133 @@ int32_t cbd_decoder_info(const cbd_decoder *d, int64_t *device_bytes, int32_t *l
 
 int32_t cbd_synchronize(cbd_decoder *d);
 
+/*
+ * Score rows: what makes them and what draws from them (besides cbd_advance, which searches a graph through them).
+ *
+ * Element types of score rows and of what they are made from.
+ */
+typedef enum cbd_dtype { CBD_F32 = 0, CBD_F16 = 1, CBD_BF16 = 2 } cbd_dtype;
+
+typedef enum cbd_activation {
+  CBD_ACT_NONE = 0,
+  CBD_ACT_RELU = 1,
+  CBD_ACT_SIGMOID = 2,
+  CBD_ACT_TANH = 3,
+  CBD_ACT_GELU = 4, /* y/2 (1 + erf(y / sqrt 2)) */
+  CBD_ACT_SILU = 5  /* y / (1 + exp(-y)) */
+} cbd_activation;
+
+/*
+ * An affine layer of the network whose outputs the decoder reads (the acoustic model in front of it, Sec. 2.2):
+ *
+ *   out[r][n] = scale * act(sum_k in[r][k] * weight[n][k] + bias[n]) + residual_scale * residual[r][n]
+ *
+ * Products are summed in fp32 and the result is rounded once, to the output's type.  Label priors and an acoustic scale
+ * go into bias and scale, so that the fp32 rows of an output layer are what cbd_advance takes.
+ */
+typedef struct cbd_layer cbd_layer; /* opaque; immutable; device resident */
+
+typedef struct cbd_layer_desc {
+  int32_t in_features;   /* 1 .. 65536 */
+  int32_t out_features;  /* 1 .. 1048576 */
+  int32_t dtype;         /* cbd_dtype of the weights and of the inputs the layer will be applied to */
+  int32_t activation;    /* cbd_activation */
+  const void *weight;    /* DEVICE [out_features] rows of in_features elements */
+  int64_t weight_stride; /* elements from row to row, >= in_features; 0 = in_features */
+  const float *bias;     /* DEVICE [out_features], or NULL = none */
+} cbd_layer_desc;
+
+/*
+ * Lays the weights out on the current HIP device, on `hip_stream` (a hipStream_t of that device, NULL = the null stream),
+ * and waits for it: the caller's arrays are free again when the call returns.  Not while the stream is being captured.
+ */
+int32_t cbd_layer_create(const cbd_layer_desc *desc, void *hip_stream, cbd_layer **out);
+/* Frees the layer; work that still uses it must have finished. */
+int32_t cbd_layer_free(cbd_layer *l);
+
+typedef struct cbd_layer_io {
+  int32_t n_channels;           /* row (channel i, frame f) of an array X is at X + i*channel_stride + f*frame_stride */
+  int32_t n_frames;             /* (elements); n_channels or n_frames = 0: nothing to do */
+  const void *input;            /* DEVICE, elements of the layer's dtype */
+  int64_t input_channel_stride; /* >= 0; rows may overlap (a context of frames spliced into one row) */
+  int64_t input_frame_stride;
+  void *output;                 /* DEVICE; its rows must overlap neither each other nor the input */
+  int64_t output_channel_stride;
+  int64_t output_frame_stride;
+  int32_t output_dtype;         /* cbd_dtype of output and residual */
+  float scale;                  /* finite */
+  const void *residual;         /* DEVICE, or NULL = none; may be the output itself (same address and strides) */
+  int64_t residual_channel_stride; /* >= 0 */
+  int64_t residual_frame_stride;
+  float residual_scale;         /* finite */
+} cbd_layer_io;
+
+/*
+ * Enqueues one application on `hip_stream` (of the layer's device).  Uses no memory besides the arguments', so calls on
+ * several streams or from several threads may overlap, and a captured call may be replayed anywhere.  Results do not
+ * depend on how often or beside what else the call runs.  Inputs and weights that are not finite give results that are
+ * not finite in the rows and columns concerned.
+ */
+int32_t cbd_layer_apply(const cbd_layer *l, const cbd_layer_io *io, void *hip_stream);
+
+/*
+ * Drawing labels: for models whose labels are produced one after the other, each from a row of scores, where a graph is
+ * not searched.  Each channel has its own list of boosted labels and an offset, added to the listed labels' scores when a
+ * row is read (the rule of Sec. 4.1 applied to labels); scores and lists are never changed by it.
+ *
+ * Rule, per row (every choice independent of thread order):
+ *   x_i = score_i, in fp32, + offset if label i is listed (one fp32 addition); -inf and NaN: the label is masked
+ *   order: larger x first, ties by lower label
+ *   weight w_i = exp((x_i - max x) / temperature); a temperature <= 0 (or NaN) keeps the first of the order only
+ *   top_k: the first top_k of the order are kept; <= 0 = all
+ *   top_p: of these the shortest beginning of the order that holds at least the share top_p of their mass, one label at
+ *          least; >= 1 (or NaN) = all
+ *   min_p: labels with w_i < min(min_p, 1) are dropped; <= 0 (or NaN) = none
+ *   label: the lowest one at which the running sum, by label, of the kept weights exceeds random * their total
+ * Weights are summed as 64-bit integers in units of 2^-(62 - ceil(log2 num_labels)).  If scores of +inf occur, their
+ * labels share the mass equally.
+ */
+typedef struct cbd_sampler cbd_sampler; /* opaque; owns the channels' lists */
+
+/* For up to num_channels lists (>= 1) over rows of num_labels scores (1 .. 1048576), on the current HIP device; all work
+ * is enqueued on `hip_stream` (a hipStream_t of that device, NULL = the null stream). */
+int32_t cbd_sampler_create(int32_t num_channels, int32_t num_labels, void *hip_stream, cbd_sampler **out);
+/* Waits for the stream, then frees. */
+int32_t cbd_sampler_free(cbd_sampler *s);
+
+/*
+ * Replaces the lists of the given channels (HOST, n_channels entries in [0, num_channels), no duplicates), laid out like
+ * those of cbd_set_contexts: labels (HOST; any order, duplicates allowed) label_idx[list_offsets[i] .. list_offsets[i+1])
+ * in [0, num_labels), offsets HOST [n_channels], finite.  Takes effect for later cbd_sample_labels calls (and later
+ * replays of captured ones).  Nothing is changed if an argument is invalid.  Not while the stream is being captured.
+ */
+int32_t cbd_sampler_set_contexts(cbd_sampler *s, const int32_t *channels, int32_t n_channels, const int32_t *label_idx,
+                                 const int32_t *list_offsets, const float *offsets);
+
+typedef struct cbd_sample_desc {
+  int32_t n;                /* rows; 0 = nothing to do */
+  int32_t dtype;            /* cbd_dtype of the scores */
+  const void *scores;       /* DEVICE; row i is at scores + i*row_stride (elements), num_labels long */
+  int64_t row_stride;       /* >= 0; rows may be the same (several draws from one) */
+  const int32_t *channels;  /* DEVICE [n]: row i uses this channel's list (repeats allowed; outside [0, num_channels): the
+                               row gives no label); NULL = channel i, n <= num_channels */
+  const float *random;      /* DEVICE [n], in [0, 1) (NaN and values below count as 0; 1 and above choose the last kept
+                               label that has weight) */
+  const float *temperature; /* DEVICE [n] or NULL = 1 */
+  const int32_t *top_k;     /* DEVICE [n] or NULL = off */
+  const float *top_p;       /* DEVICE [n] or NULL = off */
+  const float *min_p;       /* DEVICE [n] or NULL = off */
+  int32_t *labels;          /* DEVICE [n]: the label, or -1 if all labels of the row are masked */
+  float *logprobs;          /* DEVICE [n] or NULL: its log-probability among the kept labels (-inf with label -1) */
+  int32_t *kept;            /* DEVICE [n] or NULL: how many labels were kept */
+} cbd_sample_desc;
+
+/*
+ * Enqueues one draw per row.  Everything is read when the stream reaches the call (a captured call may be replayed with
+ * new values in the same arrays); no memory besides the arguments' and the lists is used.
+ */
+int32_t cbd_sample_labels(cbd_sampler *s, const cbd_sample_desc *desc);
+
 /* Runs the kernels' wave-level prefix sum and minimum on the current device against plain host loops.
  * CBD_OK, or CBD_E_HIP with the mismatch in cbd_last_error(). */
 int32_t cbd_selftest(void);

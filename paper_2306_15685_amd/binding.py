@@ -25,7 +25,13 @@ EXPORTS = [
     "cbd_set_context", "cbd_set_contexts", "cbd_contexts_create", "cbd_context_destroy", "cbd_use_contexts", "cbd_advance", "cbd_compact_records", "cbd_best_path", "cbd_best_paths", "cbd_best_paths_static", "cbd_best_paths_begin", "cbd_best_paths_finish", "cbd_best_tails", "cbd_best_tails_begin", "cbd_best_tails_finish",
     "cbd_get_fixed", "cbd_get_tokens",
     "cbd_get_records", "cbd_get_stats", "cbd_get_parts", "cbd_decoder_info", "cbd_synchronize", "cbd_selftest", "cbd_strerror", "cbd_last_error",
+    "cbd_layer_create", "cbd_layer_free", "cbd_layer_apply",
+    "cbd_sampler_create", "cbd_sampler_free", "cbd_sampler_set_contexts", "cbd_sample_labels",
 ]
+
+# cbd_dtype and cbd_activation by name
+DTYPES = {"f32": 0, "f16": 1, "bf16": 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "sigmoid": 2, "tanh": 3, "gelu": 4, "silu": 5}
 
 
 class cbd_graph_desc(C.Structure):
@@ -55,6 +61,26 @@ class cbd_stats(C.Structure):
 
     def as_dict(self):
         return {k: getattr(self, k) for k, _ in self._fields_}
+
+
+class cbd_layer_desc(C.Structure):
+    _fields_ = [("in_features", C.c_int32), ("out_features", C.c_int32), ("dtype", C.c_int32), ("activation", C.c_int32),
+                ("weight", C.c_void_p), ("weight_stride", C.c_int64), ("bias", C.c_void_p)]
+
+
+class cbd_layer_io(C.Structure):
+    _fields_ = [("n_channels", C.c_int32), ("n_frames", C.c_int32), ("input", C.c_void_p),
+                ("input_channel_stride", C.c_int64), ("input_frame_stride", C.c_int64), ("output", C.c_void_p),
+                ("output_channel_stride", C.c_int64), ("output_frame_stride", C.c_int64), ("output_dtype", C.c_int32),
+                ("scale", C.c_float), ("residual", C.c_void_p), ("residual_channel_stride", C.c_int64),
+                ("residual_frame_stride", C.c_int64), ("residual_scale", C.c_float)]
+
+
+class cbd_sample_desc(C.Structure):
+    _fields_ = [("n", C.c_int32), ("dtype", C.c_int32), ("scores", C.c_void_p), ("row_stride", C.c_int64),
+                ("channels", C.c_void_p), ("random", C.c_void_p), ("temperature", C.c_void_p), ("top_k", C.c_void_p),
+                ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("labels", C.c_void_p), ("logprobs", C.c_void_p),
+                ("kept", C.c_void_p)]
 
 
 _lib = None
@@ -136,6 +162,20 @@ def lib():
     L.cbd_strerror.argtypes = [i32]
     L.cbd_last_error.restype = C.c_char_p
     L.cbd_last_error.argtypes = []
+    L.cbd_layer_create.restype = i32
+    L.cbd_layer_create.argtypes = [C.POINTER(cbd_layer_desc), vp, C.POINTER(vp)]
+    L.cbd_layer_free.restype = i32
+    L.cbd_layer_free.argtypes = [vp]
+    L.cbd_layer_apply.restype = i32
+    L.cbd_layer_apply.argtypes = [vp, C.POINTER(cbd_layer_io), vp]
+    L.cbd_sampler_create.restype = i32
+    L.cbd_sampler_create.argtypes = [i32, i32, vp, C.POINTER(vp)]
+    L.cbd_sampler_free.restype = i32
+    L.cbd_sampler_free.argtypes = [vp]
+    L.cbd_sampler_set_contexts.restype = i32
+    L.cbd_sampler_set_contexts.argtypes = [vp, vp, i32, vp, vp, vp]
+    L.cbd_sample_labels.restype = i32
+    L.cbd_sample_labels.argtypes = [vp, C.POINTER(cbd_sample_desc)]
     _lib = L
     return L
 
@@ -490,3 +530,60 @@ def cbd_selftest():
 
 def cbd_strerror(status: int) -> str:
     return lib().cbd_strerror(int(status)).decode()
+
+
+# ---- score rows: the layers that make them, the sampler that draws from them ----
+# (*_ptr: device addresses, e.g. tensor.data_ptr(); 0 = NULL; strides in elements)
+
+def cbd_layer_create(weight_ptr: int, in_features, out_features, dtype, weight_stride=0, bias_ptr: int = 0, activation=0,
+                     hip_stream=0):
+    """dtype, activation: of DTYPES and ACTIVATIONS.  The weight and bias arrays are free again afterwards."""
+    desc = cbd_layer_desc(int(in_features), int(out_features), int(dtype), int(activation), int(weight_ptr) or None,
+                          int(weight_stride), int(bias_ptr) or None)
+    h = C.c_void_p()
+    _check(lib().cbd_layer_create(C.byref(desc), C.c_void_p(int(hip_stream)), C.byref(h)), "cbd_layer_create")
+    return h
+
+
+def cbd_layer_free(layer):
+    _check(lib().cbd_layer_free(layer), "cbd_layer_free")
+
+
+def cbd_layer_apply(layer, n_channels, n_frames, input_ptr: int, input_channel_stride, input_frame_stride, output_ptr: int,
+                    output_channel_stride, output_frame_stride, output_dtype=0, scale=1.0, residual_ptr: int = 0,
+                    residual_channel_stride=0, residual_frame_stride=0, residual_scale=1.0, hip_stream=0):
+    io = cbd_layer_io(int(n_channels), int(n_frames), int(input_ptr) or None, int(input_channel_stride), int(input_frame_stride),
+                      int(output_ptr) or None, int(output_channel_stride), int(output_frame_stride), int(output_dtype),
+                      float(scale), int(residual_ptr) or None, int(residual_channel_stride), int(residual_frame_stride),
+                      float(residual_scale))
+    _check(lib().cbd_layer_apply(layer, C.byref(io), C.c_void_p(int(hip_stream))), "cbd_layer_apply")
+
+
+def cbd_sampler_create(num_channels, num_labels, hip_stream=0):
+    h = C.c_void_p()
+    _check(lib().cbd_sampler_create(int(num_channels), int(num_labels), C.c_void_p(int(hip_stream)), C.byref(h)),
+           "cbd_sampler_create")
+    return h
+
+
+def cbd_sampler_free(s):
+    _check(lib().cbd_sampler_free(s), "cbd_sampler_free")
+
+
+def cbd_sampler_set_contexts(s, channels, lists, offsets, packed=None):
+    """lists: one array of labels per channel, or pass packed=(label_idx, list_offsets) from pack_lists."""
+    ch = _i32(channels)
+    cat, lo = packed if packed is not None else pack_lists(lists)
+    off = np.ascontiguousarray(offsets, dtype=np.float32)
+    if not (ch.size == off.size == lo.size - 1):   # (the library cannot see how long the arrays are)
+        raise ValueError("cbd_sampler_set_contexts: one list and one offset per channel")
+    _check(lib().cbd_sampler_set_contexts(s, _p(ch), int(ch.size), _p(cat), _p(lo), _p(off)), "cbd_sampler_set_contexts")
+
+
+def cbd_sample_labels(s, n, scores_ptr: int, row_stride, dtype, random_ptr: int, labels_ptr: int, channels_ptr: int = 0,
+                      temperature_ptr: int = 0, top_k_ptr: int = 0, top_p_ptr: int = 0, min_p_ptr: int = 0,
+                      logprobs_ptr: int = 0, kept_ptr: int = 0):
+    d = cbd_sample_desc(int(n), int(dtype), int(scores_ptr) or None, int(row_stride), int(channels_ptr) or None,
+                        int(random_ptr) or None, int(temperature_ptr) or None, int(top_k_ptr) or None, int(top_p_ptr) or None,
+                        int(min_p_ptr) or None, int(labels_ptr) or None, int(logprobs_ptr) or None, int(kept_ptr) or None)
+    _check(lib().cbd_sample_labels(s, C.byref(d)), "cbd_sample_labels")
