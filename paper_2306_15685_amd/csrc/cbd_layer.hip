@@ -2,6 +2,7 @@
 // include/cbd.h for the contract of each call.
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "cbd_host.hpp"
 #include "cbd_score.hpp"
@@ -20,46 +21,479 @@ struct LayerParams {
   void *out;
   int64_t x_cs, x_fs, out_cs, out_fs, res_cs, res_fs;
   int32_t rows, frames, K, N;
+  int32_t w_blocks, w_steps;   // the packed weights: blocks of 16 outputs, steps of 64 bytes along K
+  int32_t act, out_dtype;
   float scale, residual_scale;
+  uint32_t frames_mul, frames_shift;   // r / frames = r * frames_mul >> frames_shift for 0 <= r < 2^31
 };
 
-template <int kAct> __device__ __forceinline__ float activate(float y) {
-  if (kAct == CBD_ACT_RELU) return y < 0.0f ? 0.0f : y;   // (NaN stays)
-  if (kAct == CBD_ACT_SIGMOID) return 1.0f / (1.0f + expf(-y));
-  if (kAct == CBD_ACT_TANH) return tanhf(y);
-  if (kAct == CBD_ACT_GELU) return 0.5f * y * (1.0f + erff(y * 0.70710678118654752f));
-  if (kAct == CBD_ACT_SILU) return y / (1.0f + expf(-y));
-  return y;
+__device__ __forceinline__ int channel_of(const LayerParams &p, int r) {
+  return (int)((uint64_t)(uint32_t)r * p.frames_mul >> p.frames_shift);
 }
 
-template <typename T> __global__ void pack_weight_kernel(const T *src, int64_t stride, T *dst, int32_t K, int32_t N) {
-  const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
-  if (i < (int64_t)N * K) dst[i] = src[i / K * stride + i % K];
-}
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
+// 16 bytes at any element's address: global loads and stores of this size need no more alignment than that.
+typedef uint32_t uint4u __attribute__((ext_vector_type(4), aligned(2)));
 
-// The plain kernel: 16 x 16 outputs a workgroup, one each thread, operands through LDS.
-template <typename T, typename O, int kAct> __global__ __launch_bounds__(256) void layer_kernel(LayerParams p) {
-  __shared__ float xs[16][17], ws[16][17];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int64_t r = (int64_t)blockIdx.y * 16 + ty;
-  const int n = blockIdx.x * 16 + tx, nw = blockIdx.x * 16 + ty;
-  const T *x = (const T *)p.x + (r < p.rows ? r / p.frames * p.x_cs + r % p.frames * p.x_fs : 0);
-  const T *w = (const T *)p.w + (int64_t)nw * p.K;
-  float acc = 0.0f;
-  for (int k0 = 0; k0 < p.K; k0 += 16) {
-    const int k = k0 + tx;
-    xs[ty][tx] = r < p.rows && k < p.K ? (float)x[k] : 0.0f;
-    ws[ty][tx] = nw < p.N && k < p.K ? (float)w[k] : 0.0f;
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 16; ++j) acc = fmaf(xs[ty][j], ws[tx][j], acc);
-    __syncthreads();
+// A fragment is 16 bytes a lane: lane l holds row l % 16 and the (l / 16)-th 16-byte piece of a step of 64 bytes along K
+// (32 halves or 16 floats).  Both operands of a product use the same assignment of k to lanes, so the sum over the step
+// is complete whatever the order within it.
+template <typename T> struct Mma;   // kParts instructions make a step's product; part q of the pair a, b added to c
+template <> struct Mma<bf16> {
+  static constexpr int kParts = 1;
+  typedef bf16 V __attribute__((ext_vector_type(8)));
+  __device__ static float4v run(int, uint4v a, uint4v b, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
   }
-  if (r >= p.rows || n >= p.N) return;
-  const int64_t c = r / p.frames, f = r % p.frames;
-  float y = p.scale * activate<kAct>(acc + (p.bias ? p.bias[n] : 0.0f));
-  if (p.residual) y += p.residual_scale * (float)((const O *)p.residual)[c * p.res_cs + f * p.res_fs + n];
-  ((O *)p.out)[c * p.out_cs + f * p.out_fs + n] = (O)y;
+};
+template <> struct Mma<f16> {
+  static constexpr int kParts = 1;
+  typedef f16 V __attribute__((ext_vector_type(8)));
+  __device__ static float4v run(int, uint4v a, uint4v b, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+  }
+};
+template <> struct Mma<float> {
+  static constexpr int kParts = 4;
+  __device__ static float4v run(int q, uint4v a, uint4v b, float4v c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[q]), __uint_as_float(b[q]), c, 0, 0, 0);
+  }
+};
+
+// exp by the hardware's base-2 exponential: relative error about (|y| + 2) 2^-24.
+__device__ __forceinline__ float fast_exp(float y) { return __builtin_amdgcn_exp2f(y * 1.44269504088896341f); }
+__device__ __forceinline__ float fast_rcp(float y) { return __builtin_amdgcn_rcpf(y); }   // (1 unit in the last place)
+
+__device__ __forceinline__ float activate(int act, float y) {
+  switch (act) {
+    case CBD_ACT_RELU: return y < 0.0f ? 0.0f : y;   // (NaN stays)
+    case CBD_ACT_SIGMOID: return fast_rcp(1.0f + fast_exp(-y));
+    case CBD_ACT_TANH: {
+      // 1 - 2 / (exp(2y) + 1) loses digits near zero, where the odd Taylor series takes over: its next term is below
+      // 2^-26 of the value for |y| < 1/4
+      const float q = y * y;
+      const float near = y * (1.0f + q * (-1.0f / 3 + q * (2.0f / 15 + q * (-17.0f / 315 + q * (62.0f / 2835)))));
+      const float far = 1.0f - 2.0f * fast_rcp(fast_exp(2.0f * y) + 1.0f);
+      return fabsf(y) < 0.25f ? near : far;
+    }
+    case CBD_ACT_GELU: {
+      // y Phi(y); the normal tail by Abramowitz and Stegun 7.1.26 (error of erf at most 1.5e-7, and here it shrinks with
+      // the tail's exponential)
+      const float z = fabsf(y) * 0.70710678118654752f;
+      const float t = fast_rcp(1.0f + 0.3275911f * z);
+      const float poly = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+      const float tail = 0.5f * poly * fast_exp(-z * z);
+      return y * (y < 0.0f ? tail : 1.0f - tail);
+    }
+    case CBD_ACT_SILU: return y * fast_rcp(1.0f + fast_exp(-y));
+    default: return y;
+  }
+}
+
+typedef float float8v __attribute__((ext_vector_type(8)));
+
+template <int kAct, int n> __device__ __forceinline__ void activate_all(float (&v)[n]) {
+#pragma unroll
+  for (int j = 0; j < n; ++j) v[j] = activate(kAct, v[j]);
+}
+
+template <int n> __device__ __forceinline__ void activate_by(int act, float (&v)[n]) {
+  switch (act) {   // (the same for all lanes)
+    case CBD_ACT_RELU: activate_all<CBD_ACT_RELU>(v); break;
+    case CBD_ACT_SIGMOID: activate_all<CBD_ACT_SIGMOID>(v); break;
+    case CBD_ACT_TANH: activate_all<CBD_ACT_TANH>(v); break;
+    case CBD_ACT_GELU: activate_all<CBD_ACT_GELU>(v); break;
+    case CBD_ACT_SILU: activate_all<CBD_ACT_SILU>(v); break;
+    default: break;
+  }
+}
+
+// The layer's epilogue on neighbouring sums of one row: bias, activation, scale.
+template <bool kActivation, int n> __device__ __forceinline__ void finish(const LayerParams &p, float (&v)[n], const float (&bias)[n]) {
+#pragma unroll
+  for (int j = 0; j < n; ++j) v[j] += bias[j];
+  if (kActivation) activate_by(p.act, v);
+#pragma unroll
+  for (int j = 0; j < n; ++j) v[j] *= p.scale;
+}
+
+template <int n> __device__ __forceinline__ void load_bias(const LayerParams &p, int at, float (&bias)[n]) {
+#pragma unroll
+  for (int j = 0; j < n; ++j) bias[j] = p.bias && at + j < p.N ? p.bias[at + j] : 0.0f;
+}
+
+// Outputs `at` .. at + n - 1 of a row: the residual added, one rounding to the output's type, stored.  A row's end inside
+// them is stored element by element.
+template <typename O, int n> __device__ __forceinline__ void store_as(const LayerParams &p, int64_t out_row, int64_t res_row, int at, float (&v)[n]) {
+  O *out = (O *)p.out + out_row + at;
+  const O *res = p.residual ? (const O *)p.residual + res_row + at : nullptr;
+  struct __attribute__((aligned(sizeof(O)))) Some { O v[n]; };   // (vector loads and stores need no more alignment)
+  if (at + n <= p.N) {
+    if (res) {
+      const Some r = *(const Some *)res;
+#pragma unroll
+      for (int j = 0; j < n; ++j) v[j] += p.residual_scale * (float)r.v[j];
+    }
+    Some o;
+#pragma unroll
+    for (int j = 0; j < n; ++j) o.v[j] = (O)v[j];
+    *(Some *)out = o;
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < n; ++j) {
+    if (at + j < p.N) {
+      float y = v[j];
+      if (res) y += p.residual_scale * (float)res[j];
+      out[j] = (O)y;
+    }
+  }
+}
+
+template <int n> __device__ __forceinline__ void store(const LayerParams &p, int64_t out_row, int64_t res_row, int at, float (&v)[n]) {
+  if (at >= p.N) return;
+  if (p.out_dtype == CBD_F32) store_as<float>(p, out_row, res_row, at, v);
+  else if (p.out_dtype == CBD_F16) store_as<f16>(p, out_row, res_row, at, v);
+  else store_as<bf16>(p, out_row, res_row, at, v);
+}
+
+// Eight neighbouring outputs of a row that lie within it, from sums with bias, activation and scale done.
+template <typename O, bool kResidual> __device__ __forceinline__ void store_whole(const LayerParams &p, int64_t out_row, int64_t res_row, int at, float8v v) {
+  typedef O V8 __attribute__((ext_vector_type(8)));
+  typedef O V8u __attribute__((ext_vector_type(8), aligned(sizeof(O))));   // (vector accesses need no more alignment)
+  if (kResidual) {
+    const V8 r = *(const V8u *)((const O *)p.residual + res_row + at);
+    v += p.residual_scale * __builtin_convertvector(r, float8v);
+  }
+  if (sizeof(O) == 4) {
+    // fp32: a lane's eight outputs are two stores.  The four lanes of a row first exchange halves, so that each store
+    // fills 64 bytes of the row instead of every other 16 (output layer of 12800 rows, 1024 -> 6000: 181 -> 173 us).
+    float4v lo, hi;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[q]), __float_as_uint(v[q + 4]), false, false);
+      const auto b = __builtin_amdgcn_permlane32_swap(a[0], a[1], false, false);
+      lo[q] = __uint_as_float(b[0]);
+      hi[q] = __uint_as_float(b[1]);
+    }
+    typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
+    const int g = (threadIdx.x >> 4) & 3;
+    float *out = (float *)p.out + out_row + at - g * 4;
+    *(float4u *)out = lo;
+    *(float4u *)(out + 16) = hi;
+    return;
+  }
+  *(V8u *)((O *)p.out + out_row + at) = __builtin_convertvector(v, V8);   // (the one rounding to the output's type)
+}
+
+// The end of a tile kernel: a wave's FM x FN blocks of sums become outputs.  With the packed weights' order of outputs a
+// lane holds, of row lane % 16 of each row block, eight neighbouring outputs per pair of blocks, and the four lanes of a
+// row 32: one 16-byte store (two for fp32) a lane fills 64 bytes of a row.
+//
+// A tile that lies within the rows and outputs: straight-line code for layers without activation (15 instructions for
+// eight outputs), a loop over the row blocks for the others.
+template <typename O, bool kResidual, bool kActivation, int FM, int FN>
+__device__ __forceinline__ void finish_whole(const LayerParams &p, float4v (&acc)[FM][FN], const longlong2 *rows_at, int n, int lane) {
+  float bias[FN / 2][8];
+#pragma unroll
+  for (int j = 0; j < FN / 2; ++j) load_bias(p, n + j * 32, bias[j]);
+  if (!kActivation) {
+#pragma unroll
+    for (int j = 0; j < FN * 4; ++j) bias[j / 8][j % 8] *= p.scale;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) {
+      const longlong2 at = rows_at[i * 16 + (lane & 15)];
+#pragma unroll
+      for (int j = 0; j < FN / 2; ++j) {
+        float8v v;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = fmaf(acc[i][2 * j + q / 4][q % 4], p.scale, bias[j][q]);
+        store_whole<O, kResidual>(p, at.x, at.y, n + j * 32, v);
+      }
+    }
+    return;
+  }
+#pragma unroll 1
+  for (int i = 0; i < FM; ++i) {
+    float v[FN * 4];
+#pragma unroll
+    for (int k = 0; k < FM; ++k)   // (register arrays take no running index)
+      if (k == i) {
+#pragma unroll
+        for (int j = 0; j < FN * 4; ++j) v[j] = acc[k][j / 4][j % 4] + bias[j / 8][j % 8];
+      }
+    activate_by(p.act, v);
+    const longlong2 at = rows_at[i * 16 + (lane & 15)];
+#pragma unroll
+    for (int j = 0; j < FN / 2; ++j) {
+      float8v y;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) y[q] = v[j * 8 + q] * p.scale;
+      store_whole<O, kResidual>(p, at.x, at.y, n + j * 32, y);
+    }
+  }
+}
+
+template <typename O, bool kActivation, int FM, int FN>
+__device__ __forceinline__ void finish_tile(const LayerParams &p, float4v (&acc)[FM][FN], const longlong2 *rows_at, int n0, int lane, bool whole) {
+  const int n = n0 + (lane >> 4) * 8;
+  if (whole) {
+    if (p.residual) finish_whole<O, true, kActivation, FM, FN>(p, acc, rows_at, n, lane);
+    else finish_whole<O, false, kActivation, FM, FN>(p, acc, rows_at, n, lane);
+    return;
+  }
+  float bias[FN / 2][8];
+#pragma unroll
+  for (int j = 0; j < FN / 2; ++j) load_bias(p, n + j * 32, bias[j]);
+#pragma unroll 1
+  for (int i = 0; i < FM; ++i) {
+    float v[FN / 2][8];
+#pragma unroll
+    for (int k = 0; k < FM; ++k)
+      if (k == i) {
+#pragma unroll
+        for (int j = 0; j < FN * 4; ++j) v[j / 8][j % 8] = acc[k][j / 4][j % 4];
+      }
+    const longlong2 at = rows_at[i * 16 + (lane & 15)];   // (negative: beyond the last row)
+    if (at.x >= 0) {
+#pragma unroll
+      for (int j = 0; j < FN / 2; ++j) {
+        finish<kActivation>(p, v[j], bias[j]);
+        if (n + j * 32 < p.N) store_as<O>(p, at.x, at.y, n + j * 32, v[j]);
+      }
+    }
+  }
+}
+
+// Where the rows of a tile are in output and residual (elements), or a negative number beyond the last row.
+__device__ __forceinline__ void place_rows(const LayerParams &p, int row0, int count, longlong2 *rows_at) {
+  for (int i = threadIdx.x; i < count; i += blockDim.x) {
+    const int r = row0 + i;
+    longlong2 at = {-1, -1};
+    if (r < p.rows) {
+      const int c = channel_of(p, r), f = r - c * p.frames;
+      at.x = c * p.out_cs + f * p.out_fs;
+      at.y = c * p.res_cs + f * p.res_fs;
+    }
+    rows_at[i] = at;
+  }
+}
+
+// The tile of a workgroup.  Consecutive workgroups go to the chip's eight dies in turn: each die gets a contiguous run of
+// tiles, and the tiles of a run share weights and rows (eight row tiles below each other, then the next outputs).
+__device__ __forceinline__ void place_tile(int b, int tiles_m, int tiles_n, int *tile_m, int *tile_n) {
+  const int total = tiles_m * tiles_n, die = b & 7, q = total >> 3, rest = total & 7;
+  int t = die * q + min(die, rest) + (b >> 3);
+  constexpr int kGroup = 8;
+  const int group = t / (kGroup * tiles_n), first = group * kGroup, height = min(kGroup, tiles_m - first);
+  t -= group * kGroup * tiles_n;
+  *tile_m = first + t % height;
+  *tile_n = t / height;
+}
+
+// 16 bytes of an input row from element k on; beyond K there are zeros (and no reads).
+template <typename T> __device__ __forceinline__ uint4v load_piece(const T *row, int k, int K) {
+  constexpr int kElems = 16 / sizeof(T);
+  if (k + kElems <= K) {
+    const uint4u v = *(const uint4u *)(row + k);
+    return v;
+  }
+  T e[kElems];
+#pragma unroll
+  for (int j = 0; j < kElems; ++j) e[j] = k + j < K ? row[k + j] : (T)0.0f;
+  return __builtin_bit_cast(uint4v, e);
+}
+
+// Weights, packed once: block b of 16 outputs, step s: 64 lanes x 16 bytes in fragment order, so that a wave loads a
+// fragment as one contiguous kilobyte.  Zeros beyond N and K.  Two blocks share 32 outputs so that the sums of four
+// neighbouring rows of the first and of the second, which one lane holds, belong to eight neighbouring outputs: row q of
+// block b is output packed_output(b, q).
+__host__ __device__ __forceinline__ int packed_output(int b, int q) { return (b >> 1) * 32 + (q >> 2) * 8 + (b & 1) * 4 + (q & 3); }
+
+template <typename T> __global__ __launch_bounds__(256) void pack_weight_kernel(const T *src, int64_t stride, uint4v *dst, int32_t K,
+                                                                                 int32_t N, int32_t steps, int64_t total) {
+  constexpr int kElems = 16 / sizeof(T);
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;   // (block, step, lane)
+  if (i >= total) return;
+  const int lane = (int)(i & 63);
+  const int64_t bs = i >> 6;
+  const int n = packed_output((int)(bs / steps), lane & 15), k = (int)(bs % steps) * 4 * kElems + (lane >> 4) * kElems;
+  uint4v v = {0u, 0u, 0u, 0u};
+  if (n < N) v = load_piece<T>(src + (int64_t)n * stride, k, K);
+  dst[i] = v;
+}
+
+// Tiles.  A workgroup of WM x WN waves makes (WM * FM * 16) rows x (WN * FN * 16) outputs; a wave FM x FN blocks of 16 x
+// 16.  Input rows go through LDS, 128 bytes of K at a time, two buffers; weights come straight from the packed layout
+// into registers, one such step ahead.
+template <typename T, typename O, bool kActivation, int WM, int WN, int FM, int FN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LayerParams p, int tiles_m, int tiles_n) {
+  constexpr int kThreads = 64 * WM * WN, BM = WM * FM * 16, kElems = 16 / sizeof(T), kTileK = 8 * kElems;
+  constexpr int kPieces = BM * 8 / kThreads;   // 16-byte pieces of a K tile per thread
+  __shared__ uint4v lds[2][BM * 8];
+  __shared__ longlong2 rows_at[BM];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
+  int tile_m, tile_n;
+  place_tile(blockIdx.x, tiles_m, tiles_n, &tile_m, &tile_n);
+  place_rows(p, tile_m * BM, BM, rows_at);
+  // this thread's pieces of the input: rows tid / 8 + i * (threads / 8), piece tid % 8 of each K tile
+  const T *src[kPieces];
+  int dst[kPieces];
+  const int piece = tid & 7;
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int row = (tid >> 3) + i * (kThreads / 8);
+    const int r = min(tile_m * BM + row, p.rows - 1);   // (rows beyond the last repeat it and are not stored)
+    const int c = channel_of(p, r), f = r - c * p.frames;
+    src[i] = (const T *)p.x + c * p.x_cs + f * p.x_fs;
+    dst[i] = row * 8 + (piece ^ (row & 7));   // (pieces of a row swapped by row: reads of 16 rows spread over all banks)
+  }
+  // (wave and block numbers are the same in all lanes: their addresses are kept in scalar registers)
+  const uint4v *w[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    const int block = min((tile_n * WN + wn) * FN + j, p.w_blocks - 1);   // (blocks beyond the last repeat it)
+    w[j] = (const uint4v *)p.w + (int64_t)block * p.w_steps * 64;
+  }
+  float4v acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+  // A K tile is worked off in four groups: two steps of K, each in two halves of the row blocks.  While the products of a
+  // group run, the next group's rows are on their way from LDS; a step's weights are replaced by the next tile's as soon
+  // as its last product is issued; the next tile's rows wait in registers and go to the other LDS buffer ahead of the
+  // barrier, behind which the last group's products cover the first reads.
+  constexpr int G = FM / 2;
+  uint4v stage[kPieces], wv[2][FN], xa[G], xb[G];
+  const int x_at = (wm * FM * 16 + (lane & 15)) * 8, swap = lane & 7;   // (16-row blocks start at multiples of 8 rows)
+  auto read_group = [&](int t, int g, uint4v *x) {
+    const uint4v *buf = lds[t & 1] + x_at + (((g >> 1) * 4 + (lane >> 4)) ^ swap);
+#pragma unroll
+    for (int i = 0; i < G; ++i) x[i] = buf[((g & 1) * G + i) * 128];
+  };
+  auto load_weights = [&](int t, int step) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) wv[step][j] = w[j][(t * 2 + step) * 64 + lane];
+  };
+  auto products = [&](int g, const uint4v *x) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int q = 0; q < Mma<T>::kParts; ++q)   // (outermost: neighbouring products go to different sums)
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[(g & 1) * G + i][j] = Mma<T>::run(q, wv[g >> 1][j], x[i], acc[(g & 1) * G + i][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto write_stage = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) lds[t & 1][dst[i]] = stage[i];
+  };
+  auto load_whole = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) { const uint4u v = *(const uint4u *)(src[i] + t * kTileK + piece * kElems); stage[i] = v; }
+  };
+  auto load_end = [&](int t) {   // (the last tile may reach beyond K)
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) stage[i] = load_piece<T>(src[i], t * kTileK + piece * kElems, p.K);
+  };
+  const int n_tiles = p.w_steps / 2;
+  auto tile = [&](int t, auto next) {   // next: 0 = a whole tile follows, 1 = the last one follows, 2 = none
+    constexpr bool more = decltype(next)::value < 2;
+    if constexpr (decltype(next)::value == 0) load_whole(t + 1);
+    if constexpr (decltype(next)::value == 1) load_end(t + 1);
+    read_group(t, 1, xb);
+    products(0, xa);
+    read_group(t, 2, xa);
+    products(1, xb);
+    if constexpr (more) load_weights(t + 1, 0);
+    read_group(t, 3, xb);
+    products(2, xa);
+    if constexpr (more) {
+      write_stage(t + 1);
+      __syncthreads();
+      read_group(t + 1, 0, xa);
+    }
+    products(3, xb);
+    if constexpr (more) load_weights(t + 1, 1);
+  };
+  load_end(0);
+  load_weights(0, 0);
+  load_weights(0, 1);
+  write_stage(0);
+  __syncthreads();
+  read_group(0, 0, xa);
+  int t = 0;
+  for (; t < n_tiles - 2; ++t) tile(t, std::integral_constant<int, 0>());
+  if (n_tiles > 1) tile(t++, std::integral_constant<int, 1>());
+  tile(t, std::integral_constant<int, 2>());
+  finish_tile<O, kActivation>(p, acc, rows_at + wm * FM * 16, (tile_n * WN + wn) * FN * 16, lane,
+                      (tile_m + 1) * BM <= p.rows && (tile_n + 1) * WN * FN * 16 <= p.N);
+}
+
+// Few rows: a workgroup makes (FM * 16) rows x 16 outputs, its waves share K (wave w takes groups of four steps w, w +
+// kWaves, ...) and add their sums up in LDS, in the order of the waves.  No operand is used twice by a wave, so both come
+// straight from memory, four steps in flight.
+constexpr int kNarrowWaves = 8;
+template <typename T, int FM> __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(LayerParams p) {
+  constexpr int kElems = 16 / sizeof(T), kStep = 4 * kElems, kAhead = 4;
+  __shared__ float4v sums[kNarrowWaves][FM][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, block = blockIdx.x;
+  const T *src[FM];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int r = min((int)(blockIdx.y * FM + i) * 16 + (lane & 15), p.rows - 1);
+    const int c = channel_of(p, r), f = r - c * p.frames;
+    src[i] = (const T *)p.x + c * p.x_cs + f * p.x_fs + (lane >> 4) * kElems;
+  }
+  const uint4v *w = (const uint4v *)p.w + (int64_t)block * p.w_steps * 64 + lane;
+  float4v acc[FM];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) acc[i] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = wave * kAhead; s0 < p.w_steps; s0 += kNarrowWaves * kAhead) {
+    uint4v wv[kAhead], xv[kAhead][FM];
+    if (s0 + kAhead <= p.w_steps && (s0 + kAhead) * kStep <= p.K) {
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        wv[a] = w[(int64_t)(s0 + a) * 64];
+#pragma unroll
+        for (int i = 0; i < FM; ++i) { const uint4u v = *(const uint4u *)(src[i] + (s0 + a) * kStep); xv[a][i] = v; }
+      }
+    } else {
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        const int s = min(s0 + a, p.w_steps - 1);
+        wv[a] = w[(int64_t)s * 64];
+        // (a step beyond the last counts as one beyond K: zeros)
+        const int k = (s0 + a) * kStep;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) xv[a][i] = load_piece<T>(src[i], k, p.K - (lane >> 4) * kElems);
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+      for (int q = 0; q < Mma<T>::kParts; ++q)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) acc[i] = Mma<T>::run(q, wv[a], xv[a][i], acc[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i) sums[wave][i][lane] = acc[i];
+  __syncthreads();
+  // a wave finishes a row block: lane l has row l % 16 and the four outputs of the block's rows 4 (l / 16) ..
+  if (wave >= FM) return;
+  float4v v = sums[0][wave][lane];
+#pragma unroll
+  for (int k = 1; k < kNarrowWaves; ++k) v += sums[k][wave][lane];
+  const int r = (int)(blockIdx.y * FM + wave) * 16 + (lane & 15), n = packed_output(block, (lane >> 4) * 4);
+  if (r >= p.rows) return;
+  const int c = channel_of(p, r), f = r - c * p.frames;
+  float y[4] = {v[0], v[1], v[2], v[3]}, bias[4];
+  load_bias(p, n, bias);
+  finish<true>(p, y, bias);
+  store(p, c * p.out_cs + f * p.out_fs, c * p.res_cs + f * p.res_fs, n, y);
 }
 
 }  // namespace
@@ -68,6 +502,7 @@ template <typename T, typename O, int kAct> __global__ __launch_bounds__(256) vo
 struct cbd_layer {
   int device = 0;
   int32_t K = 0, N = 0, dtype = 0, act = 0;
+  int32_t blocks = 0, steps = 0;   // of the packed weights
   void *w = nullptr;
   float *bias = nullptr;
 };
@@ -76,26 +511,56 @@ namespace {
 
 using cbd::LayerParams;
 
-template <typename T, typename O, int kAct> hipError_t launch(const LayerParams &p, hipStream_t st) {
-  hipLaunchKernelGGL((cbd::layer_kernel<T, O, kAct>), dim3((p.N + 15) / 16, (p.rows + 15) / 16), dim3(256), 0, st, p);
+// calls f(O(), std::bool_constant<activation>()) for the output's type and whether there is an activation
+template <typename F> void with_output(const LayerParams &p, F f) {
+  auto with_type = [&](auto o) {
+    if (p.act == CBD_ACT_NONE) f(o, std::false_type());
+    else f(o, std::true_type());
+  };
+  if (p.out_dtype == CBD_F32) with_type(0.0f);
+  else if (p.out_dtype == CBD_F16) with_type((cbd::f16)0.0f);
+  else with_type((cbd::bf16)0.0f);
+}
+
+template <typename T, int WM, int WN, int FM, int FN> hipError_t launch_tiles(const LayerParams &p, hipStream_t st) {
+  const int tiles_m = (p.rows + WM * FM * 16 - 1) / (WM * FM * 16), tiles_n = (p.N + WN * FN * 16 - 1) / (WN * FN * 16);
+  with_output(p, [&](auto o, auto act) {
+    hipLaunchKernelGGL((cbd::tile_kernel<T, decltype(o), decltype(act)::value, WM, WN, FM, FN>), dim3((unsigned)tiles_m * (unsigned)tiles_n),
+                       dim3(64 * WM * WN), 0, st, p, tiles_m, tiles_n);
+  });
   return hipGetLastError();
 }
 
-template <typename T, typename O> hipError_t launch_act(int act, const LayerParams &p, hipStream_t st) {
-  switch (act) {
-    case CBD_ACT_RELU: return launch<T, O, CBD_ACT_RELU>(p, st);
-    case CBD_ACT_SIGMOID: return launch<T, O, CBD_ACT_SIGMOID>(p, st);
-    case CBD_ACT_TANH: return launch<T, O, CBD_ACT_TANH>(p, st);
-    case CBD_ACT_GELU: return launch<T, O, CBD_ACT_GELU>(p, st);
-    case CBD_ACT_SILU: return launch<T, O, CBD_ACT_SILU>(p, st);
-    default: return launch<T, O, CBD_ACT_NONE>(p, st);
-  }
+template <typename T, int FM> hipError_t launch_narrow(const LayerParams &p, hipStream_t st) {
+  hipLaunchKernelGGL((cbd::narrow_kernel<T, FM>), dim3((unsigned)p.w_blocks, (unsigned)((p.rows + FM * 16 - 1) / (FM * 16))),
+                     dim3(64 * cbd::kNarrowWaves), 0, st, p);
+  return hipGetLastError();
 }
 
-template <typename T> hipError_t launch_out(int out, int act, const LayerParams &p, hipStream_t st) {
-  if (out == CBD_F32) return launch_act<T, float>(act, p, st);
-  if (out == CBD_F16) return launch_act<T, cbd::f16>(act, p, st);
-  return launch_act<T, cbd::bf16>(act, p, st);
+int64_t tiles_of(const LayerParams &p, int rows, int outputs) {
+  return (int64_t)((p.rows + rows - 1) / rows) * ((p.N + outputs - 1) / outputs);
+}
+
+// Which kernel.  Few outputs in all: the narrow kernel, whose waves share K, while it takes at most about two
+// workgroups per compute unit (256 of them; bf16, rows x in -> out: 64 x 1024 -> 1024 4.5 us against 7.3 with 64 x 64
+// tiles; at 512 workgroups 256 x 1024 -> 1024 7.0 / 7.4 and 231 x 771 -> 1021 10.6 / 8.2; 200 x 1024 -> 3000 14.9 / 7.8), and always for up to 32 rows, where the weights' bytes bound it.
+// Otherwise the larger the tile, the fewer reads per product, as long as the tiles fill the chip:
+//   64 x 64 below 240 tiles of 64 x 128  (512 x 1024 -> 1024: 7.6 us against 8.8 with 64 x 128)
+//   64 x 128 below 1000 such tiles       (1000 x 1024 -> 6000: 21.3; 64 x 64 26.9, 64 x 256 22.5)
+//   64 x 256 below 512 of 128 x 256      (3000 x 1024 -> 4096: 33.5; 64 x 128 36.6, 128 x 256 36.3)
+//   128 x 256 from there                 (16384 x 1024 -> 4096: 144; 64 x 256 157)
+// fp32 products take 16 times the time of bf16 ones, so that even spreading counts more than reads: 64 x 128 tiles at
+// most (1600 x 1024 -> 6000: 175 us; 64 x 64 188, 64 x 256 214).
+template <typename T> hipError_t launch(const LayerParams &p, hipStream_t st) {
+  if (p.rows <= 16 || tiles_of(p, 16, 16) <= 512) return launch_narrow<T, 1>(p, st);
+  if (p.rows <= 32 || tiles_of(p, 32, 16) <= 400) return launch_narrow<T, 2>(p, st);
+  const int64_t tiles = tiles_of(p, 64, 128);
+  if (tiles < 240) return launch_tiles<T, 2, 2, 2, 2>(p, st);
+  if constexpr (sizeof(T) == 2) {
+    if (tiles >= 1000)
+      return tiles_of(p, 128, 256) < 512 ? launch_tiles<T, 1, 4, 4, 4>(p, st) : launch_tiles<T, 1, 4, 8, 4>(p, st);
+  }
+  return launch_tiles<T, 1, 4, 4, 2>(p, st);
 }
 
 bool aligned(const void *ptr, int32_t dtype) { return ((uintptr_t)ptr & (cbd::dtype_size(dtype) - 1)) == 0; }
@@ -145,15 +610,19 @@ int32_t cbd_layer_create(const cbd_layer_desc *desc, void *hip_stream, cbd_layer
   } guard{l};
   l->device = device;
   l->K = desc->in_features; l->N = desc->out_features; l->dtype = desc->dtype; l->act = desc->activation;
-  const int64_t total = (int64_t)l->K * l->N;
-  HIPCHK(dmalloc((char **)&l->w, (size_t)total * cbd::dtype_size(l->dtype), nullptr));
+  const int32_t step = 64 / (int32_t)cbd::dtype_size(l->dtype);
+  l->blocks = (l->N + 31) / 32 * 2;
+  l->steps = (l->K + 2 * step - 1) / (2 * step) * 2;   // (tiles take two steps at a time)
+  const int64_t total = (int64_t)l->blocks * l->steps * 64;   // 16-byte pieces
+  HIPCHK(dmalloc((char **)&l->w, (size_t)total * 16, nullptr));
   const dim3 grid((unsigned)((total + 255) / 256));
+  cbd::uint4v *w = (cbd::uint4v *)l->w;
   if (l->dtype == CBD_F32)
-    hipLaunchKernelGGL(cbd::pack_weight_kernel<uint32_t>, grid, dim3(256), 0, st, (const uint32_t *)desc->weight, stride,
-                       (uint32_t *)l->w, l->K, l->N);
+    hipLaunchKernelGGL(cbd::pack_weight_kernel<float>, grid, dim3(256), 0, st, (const float *)desc->weight, stride, w, l->K, l->N, l->steps, total);
+  else if (l->dtype == CBD_F16)
+    hipLaunchKernelGGL(cbd::pack_weight_kernel<cbd::f16>, grid, dim3(256), 0, st, (const cbd::f16 *)desc->weight, stride, w, l->K, l->N, l->steps, total);
   else
-    hipLaunchKernelGGL(cbd::pack_weight_kernel<uint16_t>, grid, dim3(256), 0, st, (const uint16_t *)desc->weight, stride,
-                       (uint16_t *)l->w, l->K, l->N);
+    hipLaunchKernelGGL(cbd::pack_weight_kernel<cbd::bf16>, grid, dim3(256), 0, st, (const cbd::bf16 *)desc->weight, stride, w, l->K, l->N, l->steps, total);
   HIPCHK(hipGetLastError());
   if (desc->bias) {
     HIPCHK(dmalloc(&l->bias, (size_t)l->N, nullptr));
@@ -207,10 +676,17 @@ int32_t cbd_layer_apply(const cbd_layer *l, const cbd_layer_io *io, void *hip_st
   p.out_cs = io->output_channel_stride; p.out_fs = io->output_frame_stride;
   p.res_cs = io->residual_channel_stride; p.res_fs = io->residual_frame_stride;
   p.rows = (int32_t)rows; p.frames = io->n_frames; p.K = l->K; p.N = l->N;
+  {
+    int log2 = 0;
+    while ((int64_t)1 << log2 < m) ++log2;
+    p.frames_shift = 31 + (uint32_t)log2;   // m <= 2^log2: ceil(2^shift / m) < 2^32 is off by less than 2^(shift - 31) / r
+    p.frames_mul = (uint32_t)((((uint64_t)1 << p.frames_shift) + (uint64_t)m - 1) / (uint64_t)m);
+  }
   p.scale = io->scale; p.residual_scale = io->residual_scale;
-  if (l->dtype == CBD_F32) HIPCHK(launch_out<float>(io->output_dtype, l->act, p, st));
-  else if (l->dtype == CBD_F16) HIPCHK(launch_out<cbd::f16>(io->output_dtype, l->act, p, st));
-  else HIPCHK(launch_out<cbd::bf16>(io->output_dtype, l->act, p, st));
+  p.w_blocks = l->blocks; p.w_steps = l->steps; p.act = l->act; p.out_dtype = io->output_dtype;
+  if (l->dtype == CBD_F32) HIPCHK(launch<float>(p, st));
+  else if (l->dtype == CBD_F16) HIPCHK(launch<cbd::f16>(p, st));
+  else HIPCHK(launch<cbd::bf16>(p, st));
   return CBD_OK;
 } catch (const std::exception &e) {
   return fail(CBD_E_HIP, std::string("layer_apply: ") + e.what());

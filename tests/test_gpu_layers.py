@@ -65,6 +65,32 @@ SHAPES = [(1, 1, 1, 1), (1, 1, 64, 16), (1, 1, 1024, 6000), (1, 3, 7, 5), (3, 1,
           (32, 33, 256, 511), (11, 97, 264, 1032), (16, 128, 64, 600)]
 
 
+# enough rows and outputs for each size of tile, none of them a whole number of tiles: 64 x 128, 64 x 256, 128 x 256 ...
+LARGE = [(1, 1003, 40, 2001), (5, 501, 72, 3301), (3, 1411, 33, 4133), (70, 61, 100, 4101)]
+# ... and with every tile whole
+LARGE_WHOLE = [(2, 512, 64, 2048), (4, 640, 32, 3328), (8, 512, 96, 4352)]
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("f16", "f16"), ("f32", "f32"), ("bf16", "bf16"), ("f16", "bf16"), ("f32", "f16")])
+@pytest.mark.parametrize("shape", LARGE + LARGE_WHOLE)
+def test_whole_numbers_are_exact_in_large_products(shape, dtype, out):
+    import torch
+    C, F, K, N = shape
+    print(dtype, out, shape, flush=True)
+    g = gen(K)
+    x, w, b = whole((C, F, K), dtype, g, 2), whole((N, K), dtype, g, 2), whole((N,), "f32", g, 9)
+    res = whole((C, F, N), out, g, 9)
+    base = (x.reshape(-1, K).double() @ w.double().t()).reshape(C, F, N) + b.double()
+    for act, residual in (("none", None), ("relu", res), ("none", res), ("relu", None)):
+        layer = Layer(w, b, dtype, act)
+        got = layer.apply(x, torch.full((C, F, N), 7.0, device=DEV, dtype=T(out)), 0.5, residual, 2.0)
+        want = 0.5 * (base.clamp(min=0) if act == "relu" else base)
+        if residual is not None:
+            want = want + 2.0 * residual.double()
+        assert torch.equal(got, want.float().to(T(out))), (shape, act)
+        layer.close()
+
+
 @pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("f16", "f32"), ("f32", "f32"), ("bf16", "bf16"), ("f16", "f16"), ("f32", "bf16"), ("f32", "f16"), ("bf16", "f16")])
 def test_whole_numbers_are_exact(dtype, out):
     import torch
