@@ -469,7 +469,7 @@ int32_t cbd_layer_apply(const cbd_layer *l, const cbd_layer_io *io, void *hip_st
  *          least; >= 1 (or NaN) = all
  *   min_p: labels with w_i < min(min_p, 1) are dropped; <= 0 (or NaN) = none
  *   label: the lowest one at which the running sum, by label, of the kept weights exceeds random * their total
- * Weights are summed as 64-bit integers in units of 2^-(62 - ceil(log2 num_labels)).  If scores of +inf occur, their
+ * Weights are summed as 64-bit integers in units of 2^-min(50, 62 - ceil(log2 num_labels)).  If scores of +inf occur, their
  * labels share the mass equally.
  */
 typedef struct cbd_sampler cbd_sampler; /* opaque; owns the channels' lists */

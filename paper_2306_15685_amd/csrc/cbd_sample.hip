@@ -3,6 +3,7 @@
 #include <cmath>
 #include <cstring>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "cbd_host.hpp"
@@ -28,191 +29,438 @@ struct SampleParams {
   int32_t unit_bits;         // weights are summed in units of 2^-unit_bits
 };
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;   // of the kernels that set lists
+constexpr uint32_t kAllTies = 0xFFFFFFFFu;
 
 // Order of scores as unsigned integers: larger score, larger key; 0 = masked (-inf or NaN); -0 is +0.
 __device__ __forceinline__ uint32_t score_key(float x) {
-  if (!(x > -__builtin_inff())) return 0u;
   const uint32_t b = __float_as_uint(x + 0.0f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
+  const uint32_t k = (int32_t)b < 0 ? ~b : b | 0x80000000u;
+  return x > -__builtin_inff() ? k : 0u;
 }
-__device__ __forceinline__ float key_score(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+__device__ __forceinline__ float key_score(uint32_t k) { return __uint_as_float((int32_t)k < 0 ? k ^ 0x80000000u : ~k); }
 
-template <typename T> struct Row {
-  const T *scores;
-  const uint32_t *bits;
-  float offset;
-  __device__ __forceinline__ uint32_t key(int i) const {
-    float x = (float)scores[i];
-    if (bits[i >> 5] >> (i & 31) & 1u) x += offset;
-    return score_key(x);
-  }
-};
-
-// Weights as integers: exp((x - best) / temperature) in units of 2^-unit_bits.
+// Weights as integers: exp((x - best) / temperature) in units of 2^-unit_bits, with relative error below 2^-36.
 struct Weigher {
-  double best, inv_t, unit;
-  __device__ __forceinline__ double log_weight(uint32_t key) const {
+  double best, inv_t, slope, bits;   // slope = log2(e) / temperature
+  __device__ __forceinline__ double distance(uint32_t key) const {
     const double x = (double)key_score(key);
-    return x == best ? 0.0 : (x - best) * inv_t;
+    return x == best ? 0.0 : x - best;   // (both may be +inf)
   }
-  __device__ __forceinline__ uint64_t units(double w) const { return __double2ull_rn(w * unit); }
+  __device__ __forceinline__ double log_weight(uint32_t key) const { return distance(key) * inv_t; }
+  // 2^y as 2^n 2^f, |f| <= 1/2, by the exponential series up to f^9 (the next term is below 2^-37)
+  __device__ __forceinline__ uint64_t units(uint32_t key) const {
+    const double y = fma(distance(key), slope, bits), n = rint(y), f = y - n;
+    double e = 1.0178086009239699e-07;   // ln(2)^k / k!
+    e = fma(e, f, 1.3215486790144307e-06);
+    e = fma(e, f, 1.5252733804059840e-05);
+    e = fma(e, f, 1.5403530393381608e-04);
+    e = fma(e, f, 1.3333558146428443e-03);
+    e = fma(e, f, 9.6181291076284770e-03);
+    e = fma(e, f, 5.5504108664821580e-02);
+    e = fma(e, f, 2.4022650695910072e-01);
+    e = fma(e, f, 6.9314718055994530e-01);
+    e = fma(e, f, 1.0);
+    // (at most 2^50: adding 2^52 leaves the nearest whole number in the low bits)
+    const double v = ldexp(e, (int)n) + 4503599627370496.0;
+    return __double_as_longlong(v) & 0x000FFFFFFFFFFFFFll;
+  }
 };
 
-template <typename V, typename Op> __device__ V block_reduce(V v, V *lds, Op op) {
-  __syncthreads();
-  lds[threadIdx.x] = v;
-  __syncthreads();
-  for (int s = kThreads / 2; s > 0; s >>= 1) {
-    if ((int)threadIdx.x < s) lds[threadIdx.x] = op(lds[threadIdx.x], lds[threadIdx.x + s]);
-    __syncthreads();
+template <typename V> __device__ __forceinline__ V wave_scan(V v, int lane) {   // inclusive sum
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const V o = __shfl_up(v, s);
+    if (lane >= s) v += o;
   }
-  v = lds[0];
-  __syncthreads();
+  return v;
+}
+template <typename V, typename Op> __device__ __forceinline__ V wave_reduce(V v, Op op) {
+#pragma unroll
+  for (int s = 32; s > 0; s >>= 1) v = op(v, __shfl_xor(v, s));
   return v;
 }
 
-template <typename T> __global__ __launch_bounds__(kThreads) void sample_kernel(SampleParams p) {
-  __shared__ uint64_t red[kThreads];
-  __shared__ uint64_t hist_mass[256];
-  __shared__ uint32_t hist_count[256];
-  __shared__ uint64_t pick[4];
-  const int r = blockIdx.x, tid = threadIdx.x, N = p.num_labels;
+// One row of scores as a workgroup reads it: kVec neighbouring labels per thread and turn; a wave's turns lie behind one
+// another, and the waves' parts too, so that (wave, turn, lane, place) is the labels' order.
+template <typename T> struct Row {
+  static constexpr int kVec = 16 / sizeof(T);
+  const T *scores;
+  const uint32_t *bits;   // of the channel's list, or NULL
+  float offset;
+  int labels;
+  __device__ __forceinline__ void load(int first, uint32_t (&key)[kVec]) const {
+    T e[kVec];
+    if (first + kVec <= labels) {
+      struct __attribute__((aligned(sizeof(T)))) Some { T v[kVec]; };   // (vector loads need no more alignment)
+      const Some s = *(const Some *)(scores + first);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) e[j] = s.v[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) e[j] = first + j < labels ? scores[first + j] : (T)-__builtin_inff();
+    }
+    uint32_t listed = 0;
+    if (bits && first < labels) listed = bits[first >> 5] >> (first & 31);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      float x = (float)e[j];
+      if (bits) x = listed >> j & 1 ? x + offset : x;
+      key[j] = score_key(x);
+    }
+  }
+};
+
+// A workgroup of kBlock threads per row.  kHeld: the row is read once and kept as keys in LDS (every thread reads its own
+// again); otherwise it is read again for each step.
+//
+// The kept labels are always a beginning of the order, so they are described by a key and a number of labels that have
+// just this key ("keys above `cut`, and the first `ties` labels with it").  top_k and top_p find them by histograms over
+// the interval of keys in question, one bin a thread: counts or masses per bin, their running sum from the best key
+// down, and the bin where it passes the border is the next interval, narrowed to the keys that occur in it, until one
+// key is left.  All sums are of integers, so their order does not matter.
+template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
+  constexpr int kWaves = kBlock / 64, kVec = Row<T>::kVec, kAhead = kHeld ? 1 : 4, kMaxCells = 32;
+  extern __shared__ uint4 held[];   // kHeld: the row's keys, by label
+  __shared__ uint64_t bins[kBlock];
+  __shared__ uint64_t cell_mass[kWaves * kMaxCells], wave_mass[kWaves];
+  __shared__ uint32_t cell_ties[kWaves * kMaxCells], wave_a[kWaves], wave_b[kWaves];
+  __shared__ uint64_t pick_before;
+  __shared__ uint32_t pick_bin;
+  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = p.num_labels;
   const int ch = p.channels ? p.channels[r] : r;
-  auto write = [&](int label, float lp, int kept) {
-    if (tid == 0) {
-      p.labels[r] = label;
-      if (p.logprobs) p.logprobs[r] = lp;
-      if (p.kept) p.kept[r] = kept;
+  auto write = [&](int label, float lp, int kept) {   // (by one thread)
+    p.labels[r] = label;
+    if (p.logprobs) p.logprobs[r] = lp;
+    if (p.kept) p.kept[r] = kept;
+  };
+  if (ch < 0 || ch >= p.num_channels) {
+    if (tid == 0) write(-1, -__builtin_inff(), 0);
+    return;
+  }
+  const float temperature = p.temperature ? p.temperature[r] : 1.0f;
+  const int k = p.top_k ? p.top_k[r] : 0;
+  const float top_p = p.top_p ? p.top_p[r] : 1.0f, min_p = p.min_p ? p.min_p[r] : 0.0f;
+  float random = p.random[r];
+  Row<T> row{(const T *)p.scores + (int64_t)r * p.row_stride, nullptr, p.offsets[ch], N};
+  if (row.offset != 0.0f) row.bits = p.bits + (int64_t)ch * p.words;
+  const int turns = (N + kBlock * kVec - 1) / (kBlock * kVec);
+  const int first = (wave * turns * 64 + lane) * kVec;   // of turn 0
+  if constexpr (kHeld) {
+    for (int t = 0; t < turns; ++t) {
+      uint32_t key[kVec];
+      row.load(first + t * 64 * kVec, key);
+#pragma unroll
+      for (int q = 0; q < kVec / 4; ++q) held[(first + t * 64 * kVec) / 4 + q] = make_uint4(key[4 * q], key[4 * q + 1], key[4 * q + 2], key[4 * q + 3]);
+    }
+  }
+  // the thread's keys of turn t
+  auto load_turn = [&](int t, uint32_t (&key)[kVec]) {
+    if constexpr (kHeld) {
+#pragma unroll
+      for (int q = 0; q < kVec / 4; ++q) {
+        const uint4 v = held[(first + t * 64 * kVec) / 4 + q];
+        key[4 * q] = v.x; key[4 * q + 1] = v.y; key[4 * q + 2] = v.z; key[4 * q + 3] = v.w;
+      }
+    } else {
+      row.load(t < turns ? first + t * 64 * kVec : N, key);   // (turns beyond the last: all masked)
     }
   };
-  if (ch < 0 || ch >= p.num_channels) { write(-1, -__builtin_inff(), 0); return; }
-  const Row<T> row{(const T *)p.scores + (int64_t)r * p.row_stride, p.bits + (int64_t)ch * p.words, p.offsets[ch]};
-  auto max64 = [](uint64_t a, uint64_t b) { return a > b ? a : b; };
-  auto add64 = [](uint64_t a, uint64_t b) { return a + b; };
-  // the first of the order: largest key, then lowest label
-  uint64_t top = 0;
-  for (int i = tid; i < N; i += kThreads) top = max64(top, (uint64_t)row.key(i) << 32 | (uint32_t)~i);
-  top = block_reduce(top, red, max64);
-  const uint32_t key_best = (uint32_t)(top >> 32);
-  if (key_best == 0) { write(-1, -__builtin_inff(), 0); return; }
-  const float temperature = p.temperature ? p.temperature[r] : 1.0f;
-  if (!(temperature > 0.0f)) { write((int)~(uint32_t)top, 0.0f, 1); return; }
-  const float best = key_score(key_best);
-  const Weigher wt{(double)best, 1.0 / (double)temperature, ldexp(1.0, p.unit_bits)};
-  const uint32_t lowest = best == __builtin_inff() ? key_best : 1u;   // smaller keys are masked
-  // kept so far: keys above `cut`, and the first `ties` labels (by label) with key `cut`
-  uint32_t cut = lowest, ties = 0xFFFFFFFFu;
-  // finds the key at which the running count (by_mass false) or mass, from the best downwards, reaches `want`
-  auto descend = [&](bool by_mass, double want, uint64_t *above) {
-    uint32_t prefix = 0;
+  // f(turn, keys) for all of the thread's turns
+  auto each_turn = [&](auto f) {
+#pragma unroll 1
+    for (int t = 0; t < turns; t += kAhead) {
+      uint32_t key[kAhead][kVec];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) load_turn(t + a, key[a]);
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) f(t + a, key[a]);
+    }
+  };
+  auto max32 = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
+  auto min32 = [](uint32_t a, uint32_t b) { return a < b ? a : b; };
+  // the largest and the smallest of what the waves give, to all
+  auto block_range = [&](uint32_t hi, uint32_t lo, uint32_t *hi_out, uint32_t *lo_out) {
+    hi = wave_reduce(hi, max32);
+    lo = wave_reduce(lo, min32);
+    __syncthreads();
+    if (lane == 0) { wave_a[wave] = hi; wave_b[wave] = lo; }
+    __syncthreads();
+    hi = wave_a[0]; lo = wave_b[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) { hi = max32(hi, wave_a[w]); lo = min32(lo, wave_b[w]); }
+    *hi_out = hi; *lo_out = lo;
+  };
+  // the lowest label of those for which f(key) holds, to all; N if none
+  auto lowest_label = [&](auto f) {
+    uint32_t at = (uint32_t)N;
+    each_turn([&](int t, const uint32_t (&key)[kVec]) {
+#pragma unroll
+      for (int j = kVec - 1; j >= 0; --j)
+        if (f(key[j])) at = min32(at, (uint32_t)(first + t * 64 * kVec + j));
+    });
+    uint32_t hi, lo;
+    block_range(0, at, &hi, &lo);
+    return (int)lo;
+  };
+  uint32_t best_key, last_key;
+  {
+    uint32_t hi = 0, lo = 0xFFFFFFFFu;
+    each_turn([&](int, const uint32_t (&key)[kVec]) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) { hi = max32(hi, key[j]); lo = min32(lo, key[j] - 1u); }   // (masked: 0 - 1 is the largest)
+    });
+    block_range(hi, lo, &best_key, &last_key);
+    last_key += 1u;
+  }
+  if (best_key == 0) {
+    if (tid == 0) write(-1, -__builtin_inff(), 0);
+    return;
+  }
+  if (!(temperature > 0.0f)) {
+    const int label = lowest_label([&](uint32_t key) { return key == best_key; });
+    if (tid == 0) write(label, 0.0f, 1);
+    return;
+  }
+  const float best = key_score(best_key);
+  if (best == __builtin_inff()) last_key = best_key;   // (scores of +inf leave the others no mass)
+  const Weigher wt{(double)best, 1.0 / (double)temperature, 1.4426950408889634 / (double)temperature, (double)p.unit_bits};
+  uint32_t cut = last_key, ties = kAllTies;
+
+  // The key at which the running count (kMass false) or mass, from best_key down to `lo`, reaches want(sum of all);
+  // *above receives the sum over larger keys.
+  auto descend = [&](auto by_mass, uint32_t lo, auto want_of, uint64_t *above) {
+    constexpr bool kMass = decltype(by_mass)::value;
+    uint32_t hi = best_key;
     uint64_t before = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      hist_mass[tid] = 0; hist_count[tid] = 0;
+    double want = 0.0;
+    for (bool begun = false; hi != lo || !begun; begun = true) {
+      const int width = 32 - __clz((int)((hi - lo) | 1u)), log2 = kBlock == 1024 ? 10 : 8;
+      const int shift = width > log2 ? width - log2 : 0;
       __syncthreads();
-      for (int i = tid; i < N; i += kThreads) {
-        const uint32_t k = row.key(i);
-        if (k < lowest || (shift < 24 && (k >> (shift + 8)) != (prefix >> (shift + 8)))) continue;
-        const uint32_t b = k >> shift & 255u;
-        atomicAdd(&hist_count[b], 1u);
-        if (by_mass) atomicAdd((unsigned long long *)&hist_mass[b], (unsigned long long)wt.units(exp(wt.log_weight(k))));
-      }
+      bins[tid] = 0;
       __syncthreads();
-      if (tid == 0) {
-        uint64_t run = before;
-        int b = 255, last = -1;
-        for (; b >= 0; --b) {
-          if (hist_count[b] == 0) continue;
-          last = b;
-          const uint64_t next = run + (by_mass ? hist_mass[b] : (uint64_t)hist_count[b]);
-          if ((double)next >= want) break;
-          run = next;
+      each_turn([&](int, const uint32_t (&key)[kVec]) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+          if (key[j] >= lo && key[j] <= hi) {
+            const uint32_t b = (hi - key[j]) >> shift;
+            if constexpr (kMass) {
+              const uint64_t u = wt.units(key[j]);
+              if (u) atomicAdd((unsigned long long *)&bins[b], (unsigned long long)u);
+            } else {
+              atomicAdd((uint32_t *)&bins[b], 1u);
+            }
+          }
         }
-        if (b < 0) { b = last; run -= by_mass ? hist_mass[b] : (uint64_t)hist_count[b]; }
-        pick[0] = (uint64_t)b; pick[1] = run;
+      });
+      __syncthreads();
+      const uint64_t mine = bins[tid];
+      uint64_t upto = wave_scan(mine, lane);
+      if (lane == 63) wave_mass[wave] = upto;
+      __syncthreads();
+      uint64_t all = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) upto += wave_mass[w];
+        all += wave_mass[w];
       }
+      if (!begun) want = want_of(all);
+      const double from = (double)(before + upto - mine), to = (double)(before + upto);
+      if (from < want && to >= want) { pick_bin = (uint32_t)tid; pick_before = before + upto - mine; }
       __syncthreads();
-      prefix |= (uint32_t)pick[0] << shift;
-      before = pick[1];
-      __syncthreads();
+      before = pick_before;
+      hi -= pick_bin << shift;
+      const uint32_t end = (hi - lo) >> shift ? hi - (1u << shift) + 1u : lo;
+      // the keys that occur in the bin
+      uint32_t top = 0, low = 0xFFFFFFFFu;
+      if (end != hi) {
+        each_turn([&](int, const uint32_t (&key)[kVec]) {
+#pragma unroll
+          for (int j = 0; j < kVec; ++j)
+            if (key[j] >= end && key[j] <= hi) { top = max32(top, key[j]); low = min32(low, key[j]); }
+        });
+        block_range(top, low, &hi, &lo);
+      } else {
+        lo = hi;
+      }
     }
     *above = before;
-    return prefix;
+    return hi;
   };
-  const int k = p.top_k ? p.top_k[r] : 0;
   if (k > 0 && k < N) {
     uint64_t above = 0;
-    uint64_t valid = 0;
-    for (int i = tid; i < N; i += kThreads) valid += row.key(i) >= lowest;
-    valid = block_reduce(valid, red, add64);
-    if ((uint64_t)k < valid) {
-      cut = descend(false, (double)k, &above);
-      ties = (uint32_t)((uint64_t)k - above);
-    }
+    bool cuts = true;
+    const uint32_t c = descend(std::false_type(), last_key, [&](uint64_t all) {
+      cuts = (uint64_t)k < all;
+      return cuts ? (double)k : (double)all;   // (fewer labels than that: nothing is cut)
+    }, &above);
+    if (cuts) { cut = c; ties = (uint32_t)((uint64_t)k - above); }
   }
-  // mass and number of what is kept: keys above `cut`, and ties
-  auto kept_mass = [&](double min_weight, uint64_t *mass, uint64_t *count, uint64_t *n_ties) {
-    uint64_t m = 0, c = 0, t = 0;
-    for (int i = tid; i < N; i += kThreads) {
-      const uint32_t key = row.key(i);
-      if (key < cut) continue;
-      const double w = exp(wt.log_weight(key));
-      if (w < min_weight) continue;
-      if (key == cut) { ++t; continue; }
-      m += wt.units(w); ++c;
-    }
-    *mass = block_reduce(m, red, add64);
-    *count = block_reduce(c, red, add64);
-    *n_ties = block_reduce(t, red, add64);
-  };
-  uint64_t mass, count, n_ties;
-  const float top_p = p.top_p ? p.top_p[r] : 1.0f;
   if (top_p <= 0.0f) {
-    cut = key_best; ties = 1;
+    cut = best_key; ties = 1;
   } else if (top_p < 1.0f) {
-    kept_mass(0.0, &mass, &count, &n_ties);
-    const uint64_t w_cut = wt.units(exp(wt.log_weight(cut)));
-    const uint64_t all = mass + (n_ties < ties ? n_ties : (uint64_t)ties) * w_cut;
-    const double want = (double)top_p * (double)all;
+    // how many labels have the key `cut` matters to the mass only if not all of them are kept
+    uint64_t left_out = 0;
+    if (ties != kAllTies) {
+      uint32_t n = 0;
+      each_turn([&](int, const uint32_t (&key)[kVec]) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) n += key[j] == cut;
+      });
+      n = wave_reduce(n, [](uint32_t a, uint32_t b) { return a + b; });
+      __syncthreads();
+      if (lane == 0) wave_a[wave] = n;
+      __syncthreads();
+      n = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) n += wave_a[w];
+      left_out = (uint64_t)(n - ties) * wt.units(cut);
+    }
     uint64_t above = 0;
-    const uint32_t c2 = descend(true, want, &above);
-    const uint64_t w2 = wt.units(exp(wt.log_weight(c2)));
-    // ties j = 0, 1, ... are kept while above + j * w2 < want
-    uint32_t t2 = 0xFFFFFFFFu;
-    if (w2 > 0) {
-      const double j = ceil((want - (double)above) / (double)w2);
-      t2 = j < 1.0 ? 1u : j < 4e9 ? (uint32_t)j : 0xFFFFFFFFu;
+    double want = 0.0;
+    const uint32_t c = descend(std::true_type(), cut, [&](uint64_t all) { return want = (double)top_p * (double)(all - left_out); }, &above);
+    // labels j = 0, 1, ... with key c are kept while above + j * (their weight) < want
+    const uint64_t w = wt.units(c);
+    uint32_t t = kAllTies;
+    if (w > 0) {
+      const double j = ceil((want - (double)above) / (double)w);
+      t = j < 1.0 ? 1u : j < 4e9 ? (uint32_t)j : kAllTies;
     }
-    if (c2 > cut) { cut = c2; ties = t2; }
-    else if (c2 == cut && t2 < ties) ties = t2;
+    if (c > cut) { cut = c; ties = t; }
+    else ties = min32(ties, t);
   }
-  const float min_p = p.min_p ? p.min_p[r] : 0.0f;
-  const double min_weight = min_p > 0.0f ? (double)fminf(min_p, 1.0f) : 0.0;
-  kept_mass(min_weight, &mass, &count, &n_ties);
-  const uint64_t w_cut = wt.units(exp(wt.log_weight(cut)));
-  const uint64_t kept_ties = n_ties < ties ? n_ties : (uint64_t)ties;
-  const uint64_t total = mass + kept_ties * w_cut;
-  float u = p.random[r];
-  if (!(u > 0.0f)) u = 0.0f;
-  uint64_t target = (uint64_t)((double)u * (double)total);
-  if (target >= total) target = total - 1;
-  // the label, found by one thread going through the row
-  if (tid == 0) {
-    uint64_t run = 0, seen = 0;
-    int label = -1;
-    uint32_t at = 0;
-    for (int i = 0; i < N; ++i) {
-      const uint32_t key = row.key(i);
-      if (key < cut) continue;
-      if (key == cut && seen++ >= ties) continue;
-      const double w = exp(wt.log_weight(key));
-      if (w < min_weight) continue;
-      run += wt.units(w);
-      if (run > target || (u == 0.0f && w > 0.0)) { label = i; at = key; break; }
+  if (min_p > 0.0f) {
+    // the smallest key with exp(log_weight) >= min_p: guessed, and found among its neighbours, 64 at a time
+    const double least = (double)fminf(min_p, 1.0f);
+    auto enough = [&](uint32_t key) { return exp(wt.log_weight(key)) >= least; };
+    const uint32_t guess = score_key((float)(wt.best + (double)temperature * log(least)));
+    uint32_t from = guess > last_key + 32u ? guess - 32u : last_key;   // lane 0's key
+    if (from > best_key) from = best_key;
+    uint64_t yes = __ballot(from + lane <= best_key && enough(min32(from + lane, best_key)));
+    if (from + 63u >= best_key) yes |= 1ull << (best_key - from);   // (the best always is)
+    if (!yes || (yes & 1ull && from > last_key)) {
+      // not there: the whole interval, a 64th of what is left at a time; lo stays a key that is not enough or last_key
+      uint32_t lo = last_key, hi = best_key;   // hi is enough
+      while (hi > lo) {
+        const uint32_t step = (hi - lo) / 64u + 1u, key = lo + (uint64_t)lane * step < hi ? lo + (uint32_t)lane * step : hi;
+        const uint64_t ok = __ballot(key == hi || enough(key));
+        const int l = __ffsll((unsigned long long)ok) - 1;
+        const uint32_t at = __shfl(key, l), under = l > 0 ? __shfl(key, l - 1) + 1u : at;
+        hi = at;
+        lo = under < hi ? under : hi;
+      }
+      from = hi;
+      yes = 1;
     }
-    p.labels[r] = label;
-    if (p.logprobs) p.logprobs[r] = (float)(wt.log_weight(at) - log((double)total / wt.unit));
-    if (p.kept) p.kept[r] = (int32_t)(count + kept_ties);
+    const uint32_t c = from + (uint32_t)(__ffsll((unsigned long long)yes) - 1);
+    if (c > cut) { cut = c; ties = kAllTies; }
+  }
+  // Mass and ties of the kept labels per cell: a wave's turns, or a stretch of them.
+  const uint64_t w_cut = wt.units(cut);
+  const int cell_turns = (turns + kMaxCells * kAhead - 1) / (kMaxCells * kAhead) * kAhead;
+  const int cells = (turns + cell_turns - 1) / cell_turns;   // per wave
+  uint64_t mass = 0;
+  uint32_t count = 0, at_cut = 0, all_count = 0;
+  auto end_cell = [&](int cell) {
+    mass = wave_reduce(mass, [](uint64_t a, uint64_t b) { return a + b; });
+    at_cut = wave_reduce(at_cut, [](uint32_t a, uint32_t b) { return a + b; });
+    if (lane == 0) { cell_mass[wave * cells + cell] = mass; cell_ties[wave * cells + cell] = at_cut; }
+    mass = 0; at_cut = 0;
+  };
+  __syncthreads();
+  each_turn([&](int t, const uint32_t (&key)[kVec]) {
+    if (t > 0 && t % cell_turns == 0 && t < turns) end_cell(t / cell_turns - 1);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      if (key[j] > cut) { mass += wt.units(key[j]); ++count; }
+      at_cut += key[j] == cut;
+    }
+  });
+  end_cell(cells - 1);
+  all_count = wave_reduce(count, [](uint32_t a, uint32_t b) { return a + b; });
+  if (lane == 0) wave_a[wave] = all_count;
+  __syncthreads();
+  uint64_t total = 0, seen = 0;
+  for (int c = 0; c < kWaves * cells; ++c) {
+    total += cell_mass[c];
+    seen += cell_ties[c];
+  }
+  const uint64_t kept_ties = seen < ties ? seen : (uint64_t)ties;
+  total += kept_ties * w_cut;
+  uint32_t kept = (uint32_t)kept_ties;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) kept += wave_a[w];
+  auto answer = [&](int label, uint32_t key) {
+    write(label, (float)(wt.log_weight(key) - log((double)total * ldexp(1.0, -p.unit_bits))), (int)kept);
+  };
+  if (!(random > 0.0f)) {
+    // the first kept label whose weight is not zero in 64 bits
+    auto some = [&](uint32_t key) { return key >= cut && wt.log_weight(key) > -745.13; };
+    const int label = lowest_label(some);
+    each_turn([&](int t, const uint32_t (&key)[kVec]) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (key[j] >= cut && first + t * 64 * kVec + j == label) answer(label, key[j]);   // (not in turns beyond the last)
+    });
+    return;
+  }
+  uint64_t target = (uint64_t)((double)random * (double)total);
+  if (random >= 1.0f || target >= total) target = total - 1;
+  // the cell in which the running sum passes the target; its wave goes through its turns
+  uint64_t run = 0;
+  uint32_t rank = 0;   // ties before
+  auto kept_of = [&](uint32_t before, uint32_t n) {   // kept ones of n ties with `before` ahead of them
+    return before >= ties ? 0u : min32(n, ties - before);
+  };
+  int cell = 0;
+  for (;; ++cell) {
+    const uint64_t m = cell_mass[cell] + (uint64_t)kept_of(rank, cell_ties[cell]) * w_cut;
+    if (run + m > target) break;
+    run += m;
+    rank += cell_ties[cell];
+  }
+  if (wave != cell / cells) return;
+  const int t0 = cell % cells * cell_turns, t1 = min(t0 + cell_turns, turns);
+  bool found = false;
+  auto look = [&](int t, const uint32_t (&key)[kVec]) {   // (all lanes of the wave)
+    if (found) return;
+    uint64_t m = 0;
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      if (key[j] > cut) m += wt.units(key[j]);
+      n += key[j] == cut;
+    }
+    const uint64_t m_upto = wave_scan(m, lane);
+    const uint32_t n_upto = wave_scan(n, lane);
+    const uint64_t upto = run + m_upto + (uint64_t)kept_of(rank, n_upto) * w_cut;
+    const uint64_t passed = __ballot(upto > target);
+    if (passed) {
+      found = true;
+      if (lane == __ffsll((unsigned long long)passed) - 1) {
+        uint32_t before = rank + n_upto - n;
+        uint64_t sum = run + m_upto - m + (uint64_t)kept_of(rank, n_upto - n) * w_cut;
+        bool done = false;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+          if (done || key[j] < cut) continue;
+          if (key[j] == cut && before++ >= ties) continue;
+          sum += wt.units(key[j]);
+          if (sum > target) { done = true; answer(first + t * 64 * kVec + j, key[j]); }
+        }
+      }
+      return;
+    }
+    run = __shfl(upto, 63);
+    // (run counts the kept ties of this turn already; rank moves on for the next)
+    rank += __shfl(n_upto, 63);
+  };
+#pragma unroll 1
+  for (int t = t0; t < t1; ++t) {
+    uint32_t key[kVec];
+    load_turn(t, key);
+    look(t, key);
   }
 }
 
@@ -245,7 +493,32 @@ struct cbd_sampler {
 
 namespace {
 constexpr int32_t kUpload = 1 << 15;   // entries of 8 bytes per upload slot
+
+constexpr size_t kHeldBytes = 144 * 1024;   // of LDS for a row's keys (with the kernel's own 9 KB: within 160 KB)
+
+template <typename T, int kBlock> size_t held_bytes(int num_labels) {   // whole turns
+  const size_t turn = (size_t)kBlock * cbd::Row<T>::kVec;
+  return ((size_t)num_labels + turn - 1) / turn * turn * sizeof(uint32_t);
 }
+
+template <typename T, int kBlock, bool kHeld> void launch_rows(const cbd::SampleParams &p, int n, hipStream_t st) {
+  const size_t lds = kHeld ? held_bytes<T, kBlock>(p.num_labels) : 0;
+  hipLaunchKernelGGL((cbd::sample_kernel<T, kBlock, kHeld>), dim3((unsigned)n), dim3(kBlock), lds, st, p);
+}
+
+template <typename T> void launch_sample(const cbd::SampleParams &p, int n, hipStream_t st) {
+  if (p.num_labels <= 8192) launch_rows<T, 256, true>(p, n, st);
+  else if (held_bytes<T, 1024>(p.num_labels) <= kHeldBytes) launch_rows<T, 1024, true>(p, n, st);
+  else launch_rows<T, 1024, false>(p, n, st);
+}
+
+template <typename T> hipError_t allow_held() {   // on the current device
+  const hipError_t e = hipFuncSetAttribute((const void *)cbd::sample_kernel<T, 256, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kHeldBytes);
+  if (e != hipSuccess) return e;
+  return hipFuncSetAttribute((const void *)cbd::sample_kernel<T, 1024, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kHeldBytes);
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -268,11 +541,14 @@ int32_t cbd_sampler_create(int32_t num_channels, int32_t num_labels, void *hip_s
   s->words = (num_labels + 127) / 128 * 4;   // (rows of 16-byte pieces)
   int log2 = 0;
   while ((1 << log2) < num_labels) ++log2;
-  s->unit_bits = 62 - log2;   // num_labels weights of at most 1 stay below 2^63
+  s->unit_bits = std::min(50, 62 - log2);   // num_labels weights of at most 1 stay below 2^63; one of them below 2^51
   s->seen.assign((size_t)num_channels, 0);
   const size_t n = (size_t)num_channels * (size_t)s->words;
   HIPCHK(dmalloc(&s->bits, n, nullptr));
   HIPCHK(dmalloc(&s->offsets, (size_t)num_channels, nullptr));
+  HIPCHK(allow_held<float>());
+  HIPCHK(allow_held<cbd::f16>());
+  HIPCHK(allow_held<cbd::bf16>());
   HIPCHK(s->ring.init(sizeof(int2) * kUpload));
   HIPCHK(hipMemsetAsync(s->bits, 0, n * sizeof(uint32_t), st));
   HIPCHK(hipMemsetAsync(s->offsets, 0, (size_t)num_channels * sizeof(float), st));
@@ -371,10 +647,9 @@ int32_t cbd_sample_labels(cbd_sampler *s, const cbd_sample_desc *d) try {
   p.bits = s->bits; p.offsets = s->offsets;
   p.labels = d->labels; p.kept = d->kept; p.logprobs = d->logprobs;
   p.num_labels = s->N; p.num_channels = s->C; p.words = s->words; p.unit_bits = s->unit_bits;
-  const dim3 grid((unsigned)d->n), block(cbd::kThreads);
-  if (d->dtype == CBD_F32) hipLaunchKernelGGL(cbd::sample_kernel<float>, grid, block, 0, s->stream, p);
-  else if (d->dtype == CBD_F16) hipLaunchKernelGGL(cbd::sample_kernel<cbd::f16>, grid, block, 0, s->stream, p);
-  else hipLaunchKernelGGL(cbd::sample_kernel<cbd::bf16>, grid, block, 0, s->stream, p);
+  if (d->dtype == CBD_F32) launch_sample<float>(p, d->n, s->stream);
+  else if (d->dtype == CBD_F16) launch_sample<cbd::f16>(p, d->n, s->stream);
+  else launch_sample<cbd::bf16>(p, d->n, s->stream);
   HIPCHK(hipGetLastError());
   return CBD_OK;
 } catch (const std::exception &e) {

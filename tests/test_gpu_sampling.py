@@ -1,5 +1,6 @@
 """cbd_sample_labels against the rule in 64 bits (score_reference.sample_row).  Labels and counts have to be equal;
-log-probabilities are rounded to fp32 once (half a step, 2^-24) and their total is summed in units of 2^-unit_bits."""
+log-probabilities are rounded to fp32 once (half a step, 2^-24) and their total is summed in units
+of 2^-min(50, 62 - log2 labels) from weights with a relative error of 2^-36."""
 import math
 
 import numpy as np
@@ -22,8 +23,8 @@ def T(name):
 
 def logprob_error(value, num_labels):
     """Rounding to fp32, and weights off by half a unit each."""
-    bits = 62 - math.ceil(math.log2(num_labels)) if num_labels > 1 else 62
-    return 2.0 ** -24 * abs(value) + num_labels * 2.0 ** -(bits + 1) + 1e-12
+    bits = min(50, 62 - math.ceil(math.log2(num_labels)) if num_labels > 1 else 62)
+    return 2.0 ** -24 * abs(value) + num_labels * 2.0 ** -(bits + 1) + 2.0 ** -36
 
 
 class Sampler:
