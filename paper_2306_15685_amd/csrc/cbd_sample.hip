@@ -31,6 +31,7 @@ struct SampleParams {
 
 constexpr int kThreads = 256;   // of the kernels that set lists
 constexpr uint32_t kAllTies = 0xFFFFFFFFu;
+constexpr int kList = 256;
 
 // Order of scores as unsigned integers: larger score, larger key; 0 = masked (-inf or NaN); -0 is +0.
 __device__ __forceinline__ uint32_t score_key(float x) {
@@ -67,19 +68,40 @@ struct Weigher {
   }
 };
 
-template <typename V> __device__ __forceinline__ V wave_scan(V v, int lane) {   // inclusive sum
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const V o = __shfl_up(v, s);
-    if (lane >= s) v += o;
-  }
-  return v;
+// Sums and maxima over a wave's lanes by data-parallel primitives (lane l of a row of 16 takes from l - 1, - 2, ...; then
+// the rows' last lanes are handed on), 64-bit values in two halves.
+template <int kCtrl, int kRows, int kBanks> __device__ __forceinline__ uint32_t from_lanes(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, kRows, kBanks, false);
 }
-template <typename V, typename Op> __device__ __forceinline__ V wave_reduce(V v, Op op) {
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) v = op(v, __shfl_xor(v, s));
-  return v;
+template <int kCtrl, int kRows, int kBanks> __device__ __forceinline__ uint64_t from_lanes(uint64_t v) {
+  return (uint64_t)from_lanes<kCtrl, kRows, kBanks>((uint32_t)(v >> 32)) << 32 | from_lanes<kCtrl, kRows, kBanks>((uint32_t)v);
 }
+template <typename V> __device__ __forceinline__ V wave_scan(V v) {   // sum over this lane and those before
+  V s = v;
+  s += from_lanes<0x111, 0xf, 0xf>(v);
+  s += from_lanes<0x112, 0xf, 0xf>(v);
+  s += from_lanes<0x113, 0xf, 0xf>(v);
+  s += from_lanes<0x114, 0xf, 0xe>(s);
+  s += from_lanes<0x118, 0xf, 0xc>(s);
+  s += from_lanes<0x142, 0xa, 0xf>(s);
+  s += from_lanes<0x143, 0xc, 0xf>(s);
+  return s;
+}
+__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ uint64_t last_lane(uint64_t v) { return (uint64_t)last_lane((uint32_t)(v >> 32)) << 32 | last_lane((uint32_t)v); }
+template <typename V> __device__ __forceinline__ V wave_sum(V v) { return last_lane(wave_scan(v)); }
+__device__ __forceinline__ uint32_t max32(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint32_t min32(uint32_t a, uint32_t b) { return a < b ? a : b; }
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  v = max32(v, from_lanes<0x111, 0xf, 0xf>(v));
+  v = max32(v, from_lanes<0x112, 0xf, 0xf>(v));
+  v = max32(v, from_lanes<0x114, 0xf, 0xf>(v));
+  v = max32(v, from_lanes<0x118, 0xf, 0xf>(v));
+  v = max32(v, from_lanes<0x142, 0xf, 0xf>(v));
+  v = max32(v, from_lanes<0x143, 0xf, 0xf>(v));
+  return last_lane(v);
+}
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) { return ~wave_max(~v); }
 
 // One row of scores as a workgroup reads it: kVec neighbouring labels per thread and turn; a wave's turns lie behind one
 // another, and the waves' parts too, so that (wave, turn, lane, place) is the labels' order.
@@ -120,13 +142,14 @@ template <typename T> struct Row {
 // down, and the bin where it passes the border is the next interval, narrowed to the keys that occur in it, until one
 // key is left.  All sums are of integers, so their order does not matter.
 template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
-  constexpr int kWaves = kBlock / 64, kVec = Row<T>::kVec, kAhead = kHeld ? 1 : 4, kMaxCells = 32;
+  constexpr int kWaves = kBlock / 64, kVec = Row<T>::kVec, kAhead = kHeld ? 1 : 4, kMaxCells = kHeld ? 1 : 32;
   extern __shared__ uint4 held[];   // kHeld: the row's keys, by label
-  __shared__ uint64_t bins[kBlock];
+  __shared__ uint64_t bins[kBlock];   // of a histogram; later the gathered labels: key << 32 | ~label (larger: earlier in the order)
+  __shared__ uint64_t sorted[kList];  // weights of the gathered labels, in the order
   __shared__ uint64_t cell_mass[kWaves * kMaxCells], wave_mass[kWaves];
-  __shared__ uint32_t cell_ties[kWaves * kMaxCells], wave_a[kWaves], wave_b[kWaves];
+  __shared__ uint32_t cell_ties[kWaves * kMaxCells], wave_a[kWaves], wave_b[kWaves], wave_c[kWaves];
   __shared__ uint64_t pick_before;
-  __shared__ uint32_t pick_bin;
+  __shared__ uint32_t pick_bin, pick_count;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = p.num_labels;
   const int ch = p.channels ? p.channels[r] : r;
   auto write = [&](int label, float lp, int kept) {   // (by one thread)
@@ -177,12 +200,10 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       for (int a = 0; a < kAhead; ++a) f(t + a, key[a]);
     }
   };
-  auto max32 = [](uint32_t a, uint32_t b) { return a > b ? a : b; };
-  auto min32 = [](uint32_t a, uint32_t b) { return a < b ? a : b; };
   // the largest and the smallest of what the waves give, to all
   auto block_range = [&](uint32_t hi, uint32_t lo, uint32_t *hi_out, uint32_t *lo_out) {
-    hi = wave_reduce(hi, max32);
-    lo = wave_reduce(lo, min32);
+    hi = wave_max(hi);
+    lo = wave_min(lo);
     __syncthreads();
     if (lane == 0) { wave_a[wave] = hi; wave_b[wave] = lo; }
     __syncthreads();
@@ -227,14 +248,43 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   const Weigher wt{(double)best, 1.0 / (double)temperature, 1.4426950408889634 / (double)temperature, (double)p.unit_bits};
   uint32_t cut = last_key, ties = kAllTies;
 
-  // The key at which the running count (kMass false) or mass, from best_key down to `lo`, reaches want(sum of all);
-  // *above receives the sum over larger keys.
-  auto descend = [&](auto by_mass, uint32_t lo, auto want_of, uint64_t *above) {
+  // labels with keys from `floor` on, gathered by their wave and lane, for n of them at most kList (n is exact)
+  auto gather = [&](uint32_t floor) {
+    uint32_t n = 0;
+    each_turn([&](int, const uint32_t (&key)[kVec]) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) n += key[j] >= floor;
+    });
+    n = wave_sum(n);
+    __syncthreads();
+    if (lane == 0) wave_a[wave] = n;
+    __syncthreads();
+    uint32_t at = 0;
+    for (int w = 0; w < wave; ++w) at += wave_a[w];
+    each_turn([&](int t, const uint32_t (&key)[kVec]) {
+      n = 0;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) n += key[j] >= floor;
+      if (!__ballot(n != 0)) return;
+      const uint32_t upto = wave_scan(n);
+      uint32_t to = at + upto - n;
+      at += last_lane(upto);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (key[j] >= floor) bins[to++] = (uint64_t)key[j] << 32 | (uint32_t)~(first + t * 64 * kVec + j);
+    });
+    __syncthreads();
+  };
+  // The interval of keys in which the running count (kMass false) or mass, from best_key down to `lo`, reaches want(sum of
+  // all): until it is a single key, or until no more than kList labels have keys from its lower end on (*labels).
+  // *above receives the sum over keys above the interval.  Returns the lower end.
+  auto descend = [&](auto by_mass, uint32_t lo, auto want_of, uint64_t *above, uint32_t *labels) {
     constexpr bool kMass = decltype(by_mass)::value;
     uint32_t hi = best_key;
     uint64_t before = 0;
     double want = 0.0;
-    for (bool begun = false; hi != lo || !begun; begun = true) {
+    uint32_t n = kAllTies;
+    for (bool begun = false; (hi != lo || !begun) && n > kList; begun = true) {
       const int width = 32 - __clz((int)((hi - lo) | 1u)), log2 = kBlock == 1024 ? 10 : 8;
       const int shift = width > log2 ? width - log2 : 0;
       __syncthreads();
@@ -256,7 +306,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       });
       __syncthreads();
       const uint64_t mine = bins[tid];
-      uint64_t upto = wave_scan(mine, lane);
+      uint64_t upto = wave_scan(mine);
       if (lane == 63) wave_mass[wave] = upto;
       __syncthreads();
       uint64_t all = 0;
@@ -267,39 +317,131 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       }
       if (!begun) want = want_of(all);
       const double from = (double)(before + upto - mine), to = (double)(before + upto);
-      if (from < want && to >= want) { pick_bin = (uint32_t)tid; pick_before = before + upto - mine; }
+      if (from < want && to >= want) { pick_bin = (uint32_t)tid; pick_before = before + upto - mine; pick_count = (uint32_t)min((uint64_t)kAllTies, before + upto); }
       __syncthreads();
       before = pick_before;
       hi -= pick_bin << shift;
       const uint32_t end = (hi - lo) >> shift ? hi - (1u << shift) + 1u : lo;
-      // the keys that occur in the bin
-      uint32_t top = 0, low = 0xFFFFFFFFu;
-      if (end != hi) {
+      if (!kMass) n = pick_count;
+      if (end == hi || n <= kList) {
+        lo = end;
+      } else {
+        // the keys that occur in the bin, and how many labels have keys from its end on
+        uint32_t top = 0, low = 0xFFFFFFFFu, more = 0;
         each_turn([&](int, const uint32_t (&key)[kVec]) {
 #pragma unroll
-          for (int j = 0; j < kVec; ++j)
+          for (int j = 0; j < kVec; ++j) {
             if (key[j] >= end && key[j] <= hi) { top = max32(top, key[j]); low = min32(low, key[j]); }
+            more += key[j] >= end;
+          }
         });
+        if (kMass) {
+          more = wave_sum(more);
+          __syncthreads();
+          if (lane == 0) wave_c[wave] = more;
+        }
         block_range(top, low, &hi, &lo);
-      } else {
-        lo = hi;
+        if (kMass) {
+          n = 0;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) n += wave_c[w];
+        }
       }
     }
     *above = before;
-    return hi;
+    *labels = n;
+    return lo;
   };
-  if (k > 0 && k < N) {
+  auto enough = [&](uint32_t key, double least) { return exp(wt.log_weight(key)) >= least; };   // min_p's test
+  // The rest on n gathered labels: the first `most` of the order, of these those with less than `want` before them (share
+  // >= 0: want is this share of the mass of the first `most`), then min_p and the choice.
+  auto finish_list = [&](int n, uint32_t most, double share, double want) {
+    const uint64_t me = tid < n ? bins[tid] : 0;
+    const uint32_t key = (uint32_t)(me >> 32);
+    uint32_t rank = 0;
+    uint64_t w = 0;
+    if (tid < n) {
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) rank += bins[j] > me;
+      w = wt.units(key);
+      sorted[rank] = w;
+    }
+    __syncthreads();
+    const bool in_list = tid < kList;   // (waves beyond the list only keep step)
+    uint64_t v = in_list && tid < n ? sorted[tid] : 0, upto = 0;
+    if (in_list) {
+      upto = wave_scan(v);
+      if (lane == 63) wave_mass[wave] = upto;
+    }
+    __syncthreads();
+    if (in_list)
+      for (int i = 0; i < wave; ++i) upto += wave_mass[i];
+    most = min32(most, (uint32_t)n);
+    if (share >= 0.0) {
+      if (tid == (int)most - 1) pick_before = upto;
+      __syncthreads();
+      want = share * (double)pick_before;
+    }
+    // three beginnings of the order: the shortest counts
+    const double least = min_p > 0.0f ? (double)fminf(min_p, 1.0f) : 0.0;
+    const uint64_t by_mass = __ballot(tid < n && (tid == 0 || (double)(upto - v) < want));
+    const uint64_t by_min = __ballot(tid < n && (least == 0.0 || enough(key, least)));
+    __syncthreads();
+    if (in_list && lane == 0) { wave_a[wave] = __popcll(by_mass); wave_b[wave] = __popcll(by_min); }
+    __syncthreads();
+    uint32_t n_mass = 0, n_min = 0;
+#pragma unroll
+    for (int i = 0; i < kList / 64; ++i) { n_mass += wave_a[i]; n_min += wave_b[i]; }
+    const uint32_t kept = min32(most, min32(n_mass, n_min));
+    // by label
+    const bool mine = tid < n && rank < kept;
+    v = mine ? w : 0;
+    if (in_list) {
+      upto = wave_scan(v);
+      if (lane == 63) wave_mass[wave] = upto;
+    }
+    __syncthreads();
+    uint64_t total = 0;
+    for (int i = 0; i < kList / 64; ++i) {
+      if (i < wave) upto += wave_mass[i];
+      total += wave_mass[i];
+    }
+    bool chosen;
+    if (!(random > 0.0f)) {
+      const uint64_t some = __ballot(mine && wt.log_weight(key) > -745.13);   // (its weight is not zero in 64 bits)
+      __syncthreads();
+      if (in_list && lane == 0) wave_a[wave] = some ? __ffsll((unsigned long long)some) - 1 : 64;
+      __syncthreads();
+      int at = 0;
+      while (wave_a[at >> 6] == 64) at += 64;   // (the best label has weight)
+      chosen = tid == at + (int)wave_a[at >> 6];
+    } else {
+      uint64_t target = (uint64_t)((double)random * (double)total);
+      if (random >= 1.0f || target >= total) target = total - 1;
+      chosen = in_list && upto > target && upto - v <= target;
+    }
+    if (chosen)
+      write((int)~(uint32_t)me, (float)(wt.log_weight(key) - log((double)total * ldexp(1.0, -p.unit_bits))), (int)kept);
+  };
+  const bool by_count = k > 0 && k < N, by_share = top_p < 1.0f;
+  if (by_count) {
     uint64_t above = 0;
+    uint32_t n = 0;
     bool cuts = true;
     const uint32_t c = descend(std::false_type(), last_key, [&](uint64_t all) {
       cuts = (uint64_t)k < all;
       return cuts ? (double)k : (double)all;   // (fewer labels than that: nothing is cut)
-    }, &above);
+    }, &above, &n);
+    if (n <= kList) {
+      gather(c);
+      finish_list((int)n, (uint32_t)k, by_share ? (double)max(top_p, 0.0f) : -1.0, __builtin_inf());
+      return;
+    }
     if (cuts) { cut = c; ties = (uint32_t)((uint64_t)k - above); }
   }
   if (top_p <= 0.0f) {
     cut = best_key; ties = 1;
-  } else if (top_p < 1.0f) {
+  } else if (by_share) {
     // how many labels have the key `cut` matters to the mass only if not all of them are kept
     uint64_t left_out = 0;
     if (ties != kAllTies) {
@@ -308,7 +450,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
 #pragma unroll
         for (int j = 0; j < kVec; ++j) n += key[j] == cut;
       });
-      n = wave_reduce(n, [](uint32_t a, uint32_t b) { return a + b; });
+      n = wave_sum(n);
       __syncthreads();
       if (lane == 0) wave_a[wave] = n;
       __syncthreads();
@@ -318,8 +460,14 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       left_out = (uint64_t)(n - ties) * wt.units(cut);
     }
     uint64_t above = 0;
+    uint32_t n = 0;
     double want = 0.0;
-    const uint32_t c = descend(std::true_type(), cut, [&](uint64_t all) { return want = (double)top_p * (double)(all - left_out); }, &above);
+    const uint32_t c = descend(std::true_type(), cut, [&](uint64_t all) { return want = (double)top_p * (double)(all - left_out); }, &above, &n);
+    if (n <= kList) {   // (with top_k as well: it is larger than kList here, and keeps them all)
+      gather(c);
+      finish_list((int)n, kAllTies, -1.0, want);
+      return;
+    }
     // labels j = 0, 1, ... with key c are kept while above + j * (their weight) < want
     const uint64_t w = wt.units(c);
     uint32_t t = kAllTies;
@@ -333,18 +481,17 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   if (min_p > 0.0f) {
     // the smallest key with exp(log_weight) >= min_p: guessed, and found among its neighbours, 64 at a time
     const double least = (double)fminf(min_p, 1.0f);
-    auto enough = [&](uint32_t key) { return exp(wt.log_weight(key)) >= least; };
     const uint32_t guess = score_key((float)(wt.best + (double)temperature * log(least)));
     uint32_t from = guess > last_key + 32u ? guess - 32u : last_key;   // lane 0's key
     if (from > best_key) from = best_key;
-    uint64_t yes = __ballot(from + lane <= best_key && enough(min32(from + lane, best_key)));
+    uint64_t yes = __ballot(from + lane <= best_key && enough(min32(from + lane, best_key), least));
     if (from + 63u >= best_key) yes |= 1ull << (best_key - from);   // (the best always is)
     if (!yes || (yes & 1ull && from > last_key)) {
       // not there: the whole interval, a 64th of what is left at a time; lo stays a key that is not enough or last_key
       uint32_t lo = last_key, hi = best_key;   // hi is enough
       while (hi > lo) {
         const uint32_t step = (hi - lo) / 64u + 1u, key = lo + (uint64_t)lane * step < hi ? lo + (uint32_t)lane * step : hi;
-        const uint64_t ok = __ballot(key == hi || enough(key));
+        const uint64_t ok = __ballot(key == hi || enough(key, least));
         const int l = __ffsll((unsigned long long)ok) - 1;
         const uint32_t at = __shfl(key, l), under = l > 0 ? __shfl(key, l - 1) + 1u : at;
         hi = at;
@@ -355,6 +502,26 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     }
     const uint32_t c = from + (uint32_t)(__ffsll((unsigned long long)yes) - 1);
     if (c > cut) { cut = c; ties = kAllTies; }
+    if (!by_count && !by_share) {
+      // few labels are left, as a rule
+      uint32_t n = 0;
+      each_turn([&](int, const uint32_t (&key)[kVec]) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) n += key[j] >= cut;
+      });
+      n = wave_sum(n);
+      __syncthreads();
+      if (lane == 0) wave_c[wave] = n;
+      __syncthreads();
+      n = 0;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) n += wave_c[w];
+      if (n <= kList) {
+        gather(cut);
+        finish_list((int)n, kAllTies, -1.0, __builtin_inf());
+        return;
+      }
+    }
   }
   // Mass and ties of the kept labels per cell: a wave's turns, or a stretch of them.
   const uint64_t w_cut = wt.units(cut);
@@ -363,8 +530,8 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   uint64_t mass = 0;
   uint32_t count = 0, at_cut = 0, all_count = 0;
   auto end_cell = [&](int cell) {
-    mass = wave_reduce(mass, [](uint64_t a, uint64_t b) { return a + b; });
-    at_cut = wave_reduce(at_cut, [](uint32_t a, uint32_t b) { return a + b; });
+    mass = wave_sum(mass);
+    at_cut = wave_sum(at_cut);
     if (lane == 0) { cell_mass[wave * cells + cell] = mass; cell_ties[wave * cells + cell] = at_cut; }
     mass = 0; at_cut = 0;
   };
@@ -378,7 +545,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     }
   });
   end_cell(cells - 1);
-  all_count = wave_reduce(count, [](uint32_t a, uint32_t b) { return a + b; });
+  all_count = wave_sum(count);
   if (lane == 0) wave_a[wave] = all_count;
   __syncthreads();
   uint64_t total = 0, seen = 0;
@@ -432,8 +599,8 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       if (key[j] > cut) m += wt.units(key[j]);
       n += key[j] == cut;
     }
-    const uint64_t m_upto = wave_scan(m, lane);
-    const uint32_t n_upto = wave_scan(n, lane);
+    const uint64_t m_upto = wave_scan(m);
+    const uint32_t n_upto = wave_scan(n);
     const uint64_t upto = run + m_upto + (uint64_t)kept_of(rank, n_upto) * w_cut;
     const uint64_t passed = __ballot(upto > target);
     if (passed) {
@@ -452,9 +619,9 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       }
       return;
     }
-    run = __shfl(upto, 63);
+    run = last_lane(upto);
     // (run counts the kept ties of this turn already; rank moves on for the next)
-    rank += __shfl(n_upto, 63);
+    rank += last_lane(n_upto);
   };
 #pragma unroll 1
   for (int t = t0; t < t1; ++t) {
