@@ -111,24 +111,29 @@ template <typename T> struct Row {
   const uint32_t *bits;   // of the channel's list, or NULL
   float offset;
   int labels;
-  __device__ __forceinline__ void load(int first, uint32_t (&key)[kVec]) const {
-    T e[kVec];
+  struct Piece { uint4 scores; uint32_t listed; };
+  // labels first .. first + kVec - 1; those beyond the last are masked (and not read)
+  __device__ __forceinline__ Piece load(int first) const {
+    Piece p;
     if (first + kVec <= labels) {
-      struct __attribute__((aligned(sizeof(T)))) Some { T v[kVec]; };   // (vector loads need no more alignment)
-      const Some s = *(const Some *)(scores + first);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) e[j] = s.v[j];
+      struct __attribute__((aligned(sizeof(T)))) Some { uint4 v; };   // (vector loads need no more alignment)
+      p.scores = ((const Some *)(scores + first))->v;
     } else {
+      T e[kVec];
 #pragma unroll
       for (int j = 0; j < kVec; ++j) e[j] = first + j < labels ? scores[first + j] : (T)-__builtin_inff();
+      p.scores = __builtin_bit_cast(uint4, e);
     }
-    uint32_t listed = 0;
-    if (bits && first < labels) listed = bits[first >> 5] >> (first & 31);
+    p.listed = bits && first < labels ? bits[first >> 5] >> (first & 31) : 0u;
+    return p;
+  }
+  __device__ __forceinline__ void keys(const Piece &p, uint32_t (&key)[kVec]) const {
+    struct All { T v[kVec]; };
+    const All e = __builtin_bit_cast(All, p.scores);
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      float x = (float)e[j];
-      if (bits) x = listed >> j & 1 ? x + offset : x;
-      key[j] = score_key(x);
+      const float x = (float)e.v[j];
+      key[j] = score_key(p.listed >> j & 1 ? x + offset : x);
     }
   }
 };
@@ -142,14 +147,16 @@ template <typename T> struct Row {
 // down, and the bin where it passes the border is the next interval, narrowed to the keys that occur in it, until one
 // key is left.  All sums are of integers, so their order does not matter.
 template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
-  constexpr int kWaves = kBlock / 64, kVec = Row<T>::kVec, kAhead = kHeld ? 1 : 4, kMaxCells = kHeld ? 1 : 32;
+  constexpr int kWaves = kBlock / 64, kVec = Row<T>::kVec, kAhead = 4, kMaxCells = kHeld ? 1 : 32;
+  constexpr int kNear = !kHeld ? 8192 : kBlock == 1024 ? 512 : kList;
   extern __shared__ uint4 held[];   // kHeld: the row's keys, by label
   __shared__ uint64_t bins[kBlock];   // of a histogram; later the gathered labels: key << 32 | ~label (larger: earlier in the order)
-  __shared__ uint64_t sorted[kList];  // weights of the gathered labels, in the order
+  // labels near the cut, unordered (key << 32 | ~label); or the weights of the gathered labels, in the order
+  __shared__ uint64_t near[kNear];
   __shared__ uint64_t cell_mass[kWaves * kMaxCells], wave_mass[kWaves];
   __shared__ uint32_t cell_ties[kWaves * kMaxCells], wave_a[kWaves], wave_b[kWaves], wave_c[kWaves];
   __shared__ uint64_t pick_before;
-  __shared__ uint32_t pick_bin, pick_count;
+  __shared__ uint32_t pick_bin, pick_count, n_near;
   const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = p.num_labels;
   const int ch = p.channels ? p.channels[r] : r;
   auto write = [&](int label, float lp, int kept) {   // (by one thread)
@@ -172,7 +179,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   if constexpr (kHeld) {
     for (int t = 0; t < turns; ++t) {
       uint32_t key[kVec];
-      row.load(first + t * 64 * kVec, key);
+      row.keys(row.load(first + t * 64 * kVec), key);
 #pragma unroll
       for (int q = 0; q < kVec / 4; ++q) held[(first + t * 64 * kVec) / 4 + q] = make_uint4(key[4 * q], key[4 * q + 1], key[4 * q + 2], key[4 * q + 3]);
     }
@@ -186,18 +193,31 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
         key[4 * q] = v.x; key[4 * q + 1] = v.y; key[4 * q + 2] = v.z; key[4 * q + 3] = v.w;
       }
     } else {
-      row.load(t < turns ? first + t * 64 * kVec : N, key);   // (turns beyond the last: all masked)
+      row.keys(row.load(first + t * 64 * kVec), key);
     }
   };
-  // f(turn, keys) for all of the thread's turns
+  // f(turn, keys) for all of the thread's turns; rows that are read again: kAhead turns on their way
   auto each_turn = [&](auto f) {
+    if constexpr (kHeld) {
 #pragma unroll 1
-    for (int t = 0; t < turns; t += kAhead) {
-      uint32_t key[kAhead][kVec];
+      for (int t = 0; t < turns; ++t) {
+        uint32_t key[kVec];
+        load_turn(t, key);
+        f(t, key);
+      }
+    } else {
+      typename Row<T>::Piece next[kAhead];
 #pragma unroll
-      for (int a = 0; a < kAhead; ++a) load_turn(t + a, key[a]);
+      for (int a = 0; a < kAhead; ++a) next[a] = row.load(a < turns ? first + a * 64 * kVec : N);
+#pragma unroll 1
+      for (int t = 0; t < turns; ++t) {
+        uint32_t key[kVec];
+        row.keys(next[0], key);
 #pragma unroll
-      for (int a = 0; a < kAhead; ++a) f(t + a, key[a]);
+        for (int a = 1; a < kAhead; ++a) next[a - 1] = next[a];
+        next[kAhead - 1] = row.load(t + kAhead < turns ? first + (t + kAhead) * 64 * kVec : N);
+        f(t, key);
+      }
     }
   };
   // the largest and the smallest of what the waves give, to all
@@ -275,82 +295,148 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     });
     __syncthreads();
   };
-  // The interval of keys in which the running count (kMass false) or mass, from best_key down to `lo`, reaches want(sum of
-  // all): until it is a single key, or until no more than kList labels have keys from its lower end on (*labels).
-  // *above receives the sum over keys above the interval.  Returns the lower end.
-  auto descend = [&](auto by_mass, uint32_t lo, auto want_of, uint64_t *above, uint32_t *labels) {
-    constexpr bool kMass = decltype(by_mass)::value;
-    uint32_t hi = best_key;
-    uint64_t before = 0;
-    double want = 0.0;
-    uint32_t n = kAllTies;
-    for (bool begun = false; (hi != lo || !begun) && n > kList; begun = true) {
-      const int width = 32 - __clz((int)((hi - lo) | 1u)), log2 = kBlock == 1024 ? 10 : 8;
-      const int shift = width > log2 ? width - log2 : 0;
-      __syncthreads();
-      bins[tid] = 0;
-      __syncthreads();
-      each_turn([&](int, const uint32_t (&key)[kVec]) {
+  // f(key) for all of the row's labels, and for the labels in `near`
+  auto each_key = [&](auto f) {
+    each_turn([&](int, const uint32_t (&key)[kVec]) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-          if (key[j] >= lo && key[j] <= hi) {
-            const uint32_t b = (hi - key[j]) >> shift;
-            if constexpr (kMass) {
-              const uint64_t u = wt.units(key[j]);
-              if (u) atomicAdd((unsigned long long *)&bins[b], (unsigned long long)u);
-            } else {
-              atomicAdd((uint32_t *)&bins[b], 1u);
-            }
-          }
-        }
-      });
-      __syncthreads();
-      const uint64_t mine = bins[tid];
-      uint64_t upto = wave_scan(mine);
-      if (lane == 63) wave_mass[wave] = upto;
-      __syncthreads();
-      uint64_t all = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) upto += wave_mass[w];
-        all += wave_mass[w];
+      for (int j = 0; j < kVec; ++j) {
+        f(key[j]);
+        if (j & 1) __builtin_amdgcn_sched_barrier(0);
       }
-      if (!begun) want = want_of(all);
-      const double from = (double)(before + upto - mine), to = (double)(before + upto);
-      if (from < want && to >= want) { pick_bin = (uint32_t)tid; pick_before = before + upto - mine; pick_count = (uint32_t)min((uint64_t)kAllTies, before + upto); }
-      __syncthreads();
-      before = pick_before;
-      hi -= pick_bin << shift;
-      const uint32_t end = (hi - lo) >> shift ? hi - (1u << shift) + 1u : lo;
-      if (!kMass) n = pick_count;
-      if (end == hi || n <= kList) {
-        lo = end;
-      } else {
-        // the keys that occur in the bin, and how many labels have keys from its end on
-        uint32_t top = 0, low = 0xFFFFFFFFu, more = 0;
-        each_turn([&](int, const uint32_t (&key)[kVec]) {
-#pragma unroll
-          for (int j = 0; j < kVec; ++j) {
-            if (key[j] >= end && key[j] <= hi) { top = max32(top, key[j]); low = min32(low, key[j]); }
-            more += key[j] >= end;
-          }
-        });
-        if (kMass) {
-          more = wave_sum(more);
-          __syncthreads();
-          if (lane == 0) wave_c[wave] = more;
+    });
+  };
+  auto each_near = [&](auto f) {
+    for (uint32_t i = tid; i < n_near; i += kBlock) f((uint32_t)(near[i] >> 32));
+  };
+  // Keys from lo to hi, in which the running count or mass, from best_key down, reaches `want`; `before` is the sum over
+  // larger keys, `from_lo` (counts only) the number of labels with keys from lo on.
+  struct Interval { uint32_t lo, hi; uint64_t before; double want; uint32_t from_lo; };
+  // One step: bins of the interval, and the one in which the sum passes `want` becomes the interval.
+  auto narrow = [&](auto by_mass, auto each, Interval &v, auto want_of) {
+    constexpr bool kMass = decltype(by_mass)::value;
+    const int width = 32 - __clz((int)((v.hi - v.lo) | 1u)), log2 = kBlock == 1024 ? 10 : 8;
+    const int shift = width > log2 ? width - log2 : 0;
+    __syncthreads();
+    bins[tid] = 0;
+    __syncthreads();
+    each([&](uint32_t key) {
+      if (key >= v.lo && key <= v.hi) {
+        const uint32_t b = (v.hi - key) >> shift;
+        if constexpr (kMass) {
+          const uint64_t u = wt.units(key);
+          if (u) atomicAdd((unsigned long long *)&bins[b], (unsigned long long)u);
+        } else {
+          atomicAdd((uint32_t *)&bins[b], 1u);
         }
-        block_range(top, low, &hi, &lo);
-        if (kMass) {
-          n = 0;
+      }
+    });
+    __syncthreads();
+    const uint64_t mine = bins[tid];
+    uint64_t upto = wave_scan(mine);
+    if (lane == 63) wave_mass[wave] = upto;
+    __syncthreads();
+    uint64_t all = 0;
 #pragma unroll
-          for (int w = 0; w < kWaves; ++w) n += wave_c[w];
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) upto += wave_mass[w];
+      all += wave_mass[w];
+    }
+    v.want = want_of(all, v.want);
+    const double from = (double)(v.before + upto - mine), to = (double)(v.before + upto);
+    if (from < v.want && to >= v.want) {
+      pick_bin = (uint32_t)tid;
+      pick_before = v.before + upto - mine;
+      pick_count = (uint32_t)min((uint64_t)kAllTies, v.before + upto);
+    }
+    __syncthreads();
+    v.before = pick_before;
+    v.hi -= pick_bin << shift;
+    if ((v.hi - v.lo) >> shift) v.lo = v.hi - (1u << shift) + 1u;
+    v.from_lo = pick_count;
+  };
+  auto as_before = [](uint64_t, double want) { return want; };
+  // ... and down to the keys that occur in it
+  auto tighten = [&](auto each, Interval &v) {
+    uint32_t top = 0, low = 0xFFFFFFFFu;
+    each([&](uint32_t key) {
+      if (key >= v.lo && key <= v.hi) { top = max32(top, key); low = min32(low, key); }
+    });
+    block_range(top, low, &v.hi, &v.lo);
+  };
+  // Mass of the kept labels and labels at the cut per cell: a wave's turns, or a stretch of them.
+  const int cell_turns = (turns + kMaxCells - 1) / kMaxCells;
+  const int cells = (turns + cell_turns - 1) / cell_turns;   // per wave
+  uint64_t mass = 0;
+  uint32_t at_cut = 0;
+  auto end_cell = [&](int cell) {
+    mass = wave_sum(mass);
+    at_cut = wave_sum(at_cut);
+    if (lane == 0) { cell_mass[wave * cells + cell] = mass; cell_ties[wave * cells + cell] = at_cut; }
+    mass = 0; at_cut = 0;
+  };
+  auto is_cell_end = [&](int t) { return t > 0 && t % cell_turns == 0 && t < turns; };
+  // One pass that notes the labels with keys from lo to hi in `near` and sums those above per cell (wave_c: their number).
+  // False if there are more than fit.
+  auto collect = [&](uint32_t lo, uint32_t hi) {
+    __syncthreads();
+    if (tid == 0) n_near = 0;
+    __syncthreads();
+    uint32_t above = 0;
+    each_turn([&](int t, const uint32_t (&key)[kVec]) {
+      if (is_cell_end(t)) end_cell(t / cell_turns - 1);
+      uint32_t n = 0;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        if (key[j] > hi) { mass += wt.units(key[j]); ++above; }
+        n += key[j] >= lo && key[j] <= hi;
+        if (j & 1) __builtin_amdgcn_sched_barrier(0);
+      }
+      if (!__ballot(n != 0)) return;
+      const uint32_t upto = wave_scan(n), all = last_lane(upto);
+      uint32_t at = 0;
+      if (lane == 0) at = atomicAdd(&n_near, all);
+      at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + upto - n;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        if (key[j] >= lo && key[j] <= hi) {
+          if (at < (uint32_t)kNear) near[at] = (uint64_t)key[j] << 32 | (uint32_t)~(first + t * 64 * kVec + j);
+          ++at;
         }
+    });
+    end_cell(cells - 1);
+    above = wave_sum(above);
+    if (lane == 0) wave_c[wave] = above;
+    __syncthreads();
+    return n_near <= (uint32_t)kNear;
+  };
+  // Finds cut and ties from `v`, an interval of more than one step's narrowing; kMass: ties follow from the mass.
+  auto settle = [&](auto by_mass, Interval &v) {
+    constexpr bool kMass = decltype(by_mass)::value;
+    bool listed = false;
+    while (v.lo != v.hi && !listed) {
+      listed = collect(v.lo, v.hi);
+      if (!listed) {
+        tighten(each_key, v);
+        if (v.lo != v.hi) narrow(by_mass, each_key, v, as_before);
       }
     }
-    *above = before;
-    *labels = n;
-    return lo;
+    const uint32_t top = v.hi;
+    while (v.lo != v.hi) {
+      tighten(each_near, v);
+      if (v.lo != v.hi) narrow(by_mass, each_near, v, as_before);
+    }
+    uint32_t t = kAllTies;
+    const uint64_t w = wt.units(v.hi);
+    if (!kMass) {
+      t = (uint32_t)(v.want - (double)v.before);
+    } else if (w > 0) {
+      // labels j = 0, 1, ... with this key are kept while before + j * (their weight) < want
+      const double j = ceil((v.want - (double)v.before) / (double)w);
+      t = j < 1.0 ? 1u : j < 4e9 ? (uint32_t)j : kAllTies;
+    }
+    if (v.hi > cut) { cut = v.hi; ties = t; }
+    else ties = min32(ties, t);
+    return listed ? top : 0u;   // labels above this key are in the cells, those down to cut in `near`
   };
   auto enough = [&](uint32_t key, double least) { return exp(wt.log_weight(key)) >= least; };   // min_p's test
   // The rest on n gathered labels: the first `most` of the order, of these those with less than `want` before them (share
@@ -364,11 +450,11 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
 #pragma unroll 4
       for (int j = 0; j < n; ++j) rank += bins[j] > me;
       w = wt.units(key);
-      sorted[rank] = w;
+      near[rank] = w;
     }
     __syncthreads();
     const bool in_list = tid < kList;   // (waves beyond the list only keep step)
-    uint64_t v = in_list && tid < n ? sorted[tid] : 0, upto = 0;
+    uint64_t v = in_list && tid < n ? near[tid] : 0, upto = 0;
     if (in_list) {
       upto = wave_scan(v);
       if (lane == 63) wave_mass[wave] = upto;
@@ -424,32 +510,33 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       write((int)~(uint32_t)me, (float)(wt.log_weight(key) - log((double)total * ldexp(1.0, -p.unit_bits))), (int)kept);
   };
   const bool by_count = k > 0 && k < N, by_share = top_p < 1.0f;
+  uint32_t listed_from = 0;   // not 0: collect()'s sums are of larger keys, and the rest of the kept labels is in `near`
   if (by_count) {
-    uint64_t above = 0;
-    uint32_t n = 0;
+    Interval v{last_key, best_key, 0, 0.0, kAllTies};
     bool cuts = true;
-    const uint32_t c = descend(std::false_type(), last_key, [&](uint64_t all) {
+    narrow(std::false_type(), each_key, v, [&](uint64_t all, double) {
       cuts = (uint64_t)k < all;
       return cuts ? (double)k : (double)all;   // (fewer labels than that: nothing is cut)
-    }, &above, &n);
-    if (n <= kList) {
-      gather(c);
-      finish_list((int)n, (uint32_t)k, by_share ? (double)max(top_p, 0.0f) : -1.0, __builtin_inf());
+    });
+    while (v.from_lo > (uint32_t)kList && k <= kList && v.lo != v.hi) {
+      tighten(each_key, v);
+      narrow(std::false_type(), each_key, v, as_before);
+    }
+    if (v.from_lo <= (uint32_t)kList) {
+      gather(v.lo);
+      finish_list((int)v.from_lo, (uint32_t)k, by_share ? (double)max(top_p, 0.0f) : -1.0, __builtin_inf());
       return;
     }
-    if (cuts) { cut = c; ties = (uint32_t)((uint64_t)k - above); }
+    if (cuts) listed_from = settle(std::false_type(), v);
   }
   if (top_p <= 0.0f) {
-    cut = best_key; ties = 1;
+    cut = best_key; ties = 1; listed_from = 0;
   } else if (by_share) {
     // how many labels have the key `cut` matters to the mass only if not all of them are kept
     uint64_t left_out = 0;
     if (ties != kAllTies) {
       uint32_t n = 0;
-      each_turn([&](int, const uint32_t (&key)[kVec]) {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) n += key[j] == cut;
-      });
+      each_key([&](uint32_t key) { n += key == cut; });
       n = wave_sum(n);
       __syncthreads();
       if (lane == 0) wave_a[wave] = n;
@@ -459,24 +546,9 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       for (int w = 0; w < kWaves; ++w) n += wave_a[w];
       left_out = (uint64_t)(n - ties) * wt.units(cut);
     }
-    uint64_t above = 0;
-    uint32_t n = 0;
-    double want = 0.0;
-    const uint32_t c = descend(std::true_type(), cut, [&](uint64_t all) { return want = (double)top_p * (double)(all - left_out); }, &above, &n);
-    if (n <= kList) {   // (with top_k as well: it is larger than kList here, and keeps them all)
-      gather(c);
-      finish_list((int)n, kAllTies, -1.0, want);
-      return;
-    }
-    // labels j = 0, 1, ... with key c are kept while above + j * (their weight) < want
-    const uint64_t w = wt.units(c);
-    uint32_t t = kAllTies;
-    if (w > 0) {
-      const double j = ceil((want - (double)above) / (double)w);
-      t = j < 1.0 ? 1u : j < 4e9 ? (uint32_t)j : kAllTies;
-    }
-    if (c > cut) { cut = c; ties = t; }
-    else ties = min32(ties, t);
+    Interval v{cut, best_key, 0, 0.0, kAllTies};
+    narrow(std::true_type(), each_key, v, [&](uint64_t all, double) { return (double)top_p * (double)(all - left_out); });
+    listed_from = settle(std::true_type(), v);
   }
   if (min_p > 0.0f) {
     // the smallest key with exp(log_weight) >= min_p: guessed, and found among its neighbours, 64 at a time
@@ -501,7 +573,10 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       yes = 1;
     }
     const uint32_t c = from + (uint32_t)(__ffsll((unsigned long long)yes) - 1);
-    if (c > cut) { cut = c; ties = kAllTies; }
+    if (c > cut) {
+      cut = c; ties = kAllTies;
+      if (c > listed_from) listed_from = 0;   // (the sums hold labels below the cut)
+    }
     if (!by_count && !by_share) {
       // few labels are left, as a rule
       uint32_t n = 0;
@@ -523,30 +598,37 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       }
     }
   }
-  // Mass and ties of the kept labels per cell: a wave's turns, or a stretch of them.
   const uint64_t w_cut = wt.units(cut);
-  const int cell_turns = (turns + kMaxCells * kAhead - 1) / (kMaxCells * kAhead) * kAhead;
-  const int cells = (turns + cell_turns - 1) / cell_turns;   // per wave
-  uint64_t mass = 0;
-  uint32_t count = 0, at_cut = 0, all_count = 0;
-  auto end_cell = [&](int cell) {
-    mass = wave_sum(mass);
-    at_cut = wave_sum(at_cut);
-    if (lane == 0) { cell_mass[wave * cells + cell] = mass; cell_ties[wave * cells + cell] = at_cut; }
-    mass = 0; at_cut = 0;
-  };
-  __syncthreads();
-  each_turn([&](int t, const uint32_t (&key)[kVec]) {
-    if (t > 0 && t % cell_turns == 0 && t < turns) end_cell(t / cell_turns - 1);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      if (key[j] > cut) { mass += wt.units(key[j]); ++count; }
-      at_cut += key[j] == cut;
+  if (listed_from) {
+    // the cells lack the labels in `near`
+    const uint32_t n = n_near;
+    __syncthreads();
+    for (uint32_t i = tid; i < n; i += kBlock) {
+      const uint32_t key = (uint32_t)(near[i] >> 32), g = ~(uint32_t)near[i] / (64u * kVec);
+      const uint32_t cell = g / (uint32_t)turns * cells + g % (uint32_t)turns / cell_turns;
+      if (key > cut) {
+        atomicAdd((unsigned long long *)&cell_mass[cell], (unsigned long long)wt.units(key));
+        atomicAdd(&wave_c[0], 1u);
+      } else if (key == cut) {
+        atomicAdd(&cell_ties[cell], 1u);
+      }
     }
-  });
-  end_cell(cells - 1);
-  all_count = wave_sum(count);
-  if (lane == 0) wave_a[wave] = all_count;
+  } else {
+    uint32_t above = 0;
+    __syncthreads();
+    each_turn([&](int t, const uint32_t (&key)[kVec]) {
+      if (is_cell_end(t)) end_cell(t / cell_turns - 1);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        if (key[j] > cut) { mass += wt.units(key[j]); ++above; }
+        at_cut += key[j] == cut;
+        if (j & 1) __builtin_amdgcn_sched_barrier(0);
+      }
+    });
+    end_cell(cells - 1);
+    above = wave_sum(above);
+    if (lane == 0) wave_c[wave] = above;
+  }
   __syncthreads();
   uint64_t total = 0, seen = 0;
   for (int c = 0; c < kWaves * cells; ++c) {
@@ -557,7 +639,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   total += kept_ties * w_cut;
   uint32_t kept = (uint32_t)kept_ties;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) kept += wave_a[w];
+  for (int w = 0; w < kWaves; ++w) kept += wave_c[w];
   auto answer = [&](int label, uint32_t key) {
     write(label, (float)(wt.log_weight(key) - log((double)total * ldexp(1.0, -p.unit_bits))), (int)kept);
   };
@@ -568,7 +650,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     each_turn([&](int t, const uint32_t (&key)[kVec]) {
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        if (key[j] >= cut && first + t * 64 * kVec + j == label) answer(label, key[j]);   // (not in turns beyond the last)
+        if (first + t * 64 * kVec + j == label) answer(label, key[j]);
     });
     return;
   }
