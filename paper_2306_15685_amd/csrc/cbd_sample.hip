@@ -33,38 +33,48 @@ constexpr int kThreads = 256;   // of the kernels that set lists
 constexpr uint32_t kAllTies = 0xFFFFFFFFu;
 constexpr int kList = 256;
 
-// Order of scores as unsigned integers: larger score, larger key; 0 = masked (-inf or NaN); -0 is +0.
+constexpr float kLargest = 3.402823466e38f;
+
+// Order of scores as unsigned integers: larger score, larger key (-0 does not occur; masked scores are -inf).
 __device__ __forceinline__ uint32_t score_key(float x) {
-  const uint32_t b = __float_as_uint(x + 0.0f);
-  const uint32_t k = (int32_t)b < 0 ? ~b : b | 0x80000000u;
-  return x > -__builtin_inff() ? k : 0u;
+  const uint32_t b = __float_as_uint(x);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
-__device__ __forceinline__ float key_score(uint32_t k) { return __uint_as_float((int32_t)k < 0 ? k ^ 0x80000000u : ~k); }
+__device__ __forceinline__ float key_score(uint32_t k) { return __uint_as_float(k ^ (~(uint32_t)((int32_t)k >> 31) | 0x80000000u)); }
+constexpr uint32_t kLowestKey = 0x00800000u;   // of the smallest finite score
+
+// a * b + c, c in scalar registers
+__device__ __forceinline__ double fma_const(double a, double b, double c) {
+  double r;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+  return r;
+}
 
 // Weights as integers: exp((x - best) / temperature) in units of 2^-unit_bits, with relative error below 2^-36.
 struct Weigher {
   double best, inv_t, slope, bits;   // slope = log2(e) / temperature
-  __device__ __forceinline__ double distance(uint32_t key) const {
-    const double x = (double)key_score(key);
-    return x == best ? 0.0 : x - best;   // (both may be +inf)
-  }
-  __device__ __forceinline__ double log_weight(uint32_t key) const { return distance(key) * inv_t; }
-  // 2^y as 2^n 2^f, |f| <= 1/2, by the exponential series up to f^9 (the next term is below 2^-37)
-  __device__ __forceinline__ uint64_t units(uint32_t key) const {
-    const double y = fma(distance(key), slope, bits), n = rint(y), f = y - n;
-    double e = 1.0178086009239699e-07;   // ln(2)^k / k!
-    e = fma(e, f, 1.3215486790144307e-06);
-    e = fma(e, f, 1.5252733804059840e-05);
-    e = fma(e, f, 1.5403530393381608e-04);
-    e = fma(e, f, 1.3333558146428443e-03);
-    e = fma(e, f, 9.6181291076284770e-03);
-    e = fma(e, f, 5.5504108664821580e-02);
-    e = fma(e, f, 2.4022650695910072e-01);
-    e = fma(e, f, 6.9314718055994530e-01);
+  // x - best, exact; scores of +inf (the best is one then) count as the largest finite number
+  __device__ __forceinline__ double distance(float x) const { return (double)fminf(x, kLargest) - best; }
+  __device__ __forceinline__ double log_weight(float x) const { return distance(x) * inv_t; }
+  // 2^y as 2^n 2^f, |f| <= 1/2, by the exponential series up to f^9 (the next term is below 2^-37).  Adding 1.5 * 2^52
+  // leaves the nearest whole number in the low bits: of y (n is added to the exponent of 2^f) and of the weight, which is
+  // at most 2^50.  Weights below 2^-4 units are nothing, so y need not be smaller than that.  Some 20 instructions of 64
+  // bits per label: they, not the bytes, bound the passes that sum weights.
+  __device__ __forceinline__ uint64_t units(float x) const {
+    constexpr double kMagic = 6755399441055744.0;
+    const double y = fmax(fma(distance(x), slope, bits), -4.0), shifted = y + kMagic, f = y - (shifted - kMagic);
+    double e = fma_const(f, 1.0178086009239699e-07, 1.3215486790144307e-06);   // ln(2)^k / k!
+    e = fma_const(e, f, 1.5252733804059840e-05);
+    e = fma_const(e, f, 1.5403530393381608e-04);
+    e = fma_const(e, f, 1.3333558146428443e-03);
+    e = fma_const(e, f, 9.6181291076284770e-03);
+    e = fma_const(e, f, 5.5504108664821580e-02);
+    e = fma_const(e, f, 2.4022650695910072e-01);
+    e = fma_const(e, f, 6.9314718055994530e-01);
     e = fma(e, f, 1.0);
-    // (at most 2^50: adding 2^52 leaves the nearest whole number in the low bits)
-    const double v = ldexp(e, (int)n) + 4503599627370496.0;
-    return __double_as_longlong(v) & 0x000FFFFFFFFFFFFFll;
+    const uint32_t n = (uint32_t)__double_as_longlong(shifted);
+    e = __hiloint2double(__double2hiint(e) + (int)(n << 20), __double2loint(e));
+    return __double_as_longlong(e + kMagic) & 0x0007FFFFFFFFFFFFll;
   }
 };
 
@@ -103,42 +113,80 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 }
 __device__ __forceinline__ uint32_t wave_min(uint32_t v) { return ~wave_max(~v); }
 
+// f(j) for j = 0 .. n - 1
+template <int n, typename F> __device__ __forceinline__ void each_of(F f) {
+#pragma unroll
+  for (int j = 0; j < n; ++j) {
+    f(j);
+    if (j & 1) __builtin_amdgcn_sched_barrier(0);   // (weights of more labels at once would need too many registers)
+  }
+}
+
 // One row of scores as a workgroup reads it: kVec neighbouring labels per thread and turn; a wave's turns lie behind one
 // another, and the waves' parts too, so that (wave, turn, lane, place) is the labels' order.
-template <typename T> struct Row {
-  static constexpr int kVec = 16 / sizeof(T);
+template <typename T, int kVec> struct Row {
+  static constexpr int kWords = kVec * (int)sizeof(T) / 4;
+  typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
+  typedef uint32_t Unaligned __attribute__((ext_vector_type(kWords), aligned(sizeof(T))));   // (vector loads need no more)
   const T *scores;
   const uint32_t *bits;   // of the channel's list, or NULL
   float offset;
   int labels;
-  struct Piece { uint4 scores; uint32_t listed; };
+  struct Piece { Words scores; uint32_t listed; };
   // labels first .. first + kVec - 1; those beyond the last are masked (and not read)
   __device__ __forceinline__ Piece load(int first) const {
     Piece p;
     if (first + kVec <= labels) {
-      struct __attribute__((aligned(sizeof(T)))) Some { uint4 v; };   // (vector loads need no more alignment)
-      p.scores = ((const Some *)(scores + first))->v;
+      p.scores = *(const Unaligned *)(scores + first);
     } else {
       T e[kVec];
 #pragma unroll
       for (int j = 0; j < kVec; ++j) e[j] = first + j < labels ? scores[first + j] : (T)-__builtin_inff();
-      p.scores = __builtin_bit_cast(uint4, e);
+      p.scores = __builtin_bit_cast(Words, e);
     }
     p.listed = bits && first < labels ? bits[first >> 5] >> (first & 31) : 0u;
     return p;
   }
-  __device__ __forceinline__ void keys(const Piece &p, uint32_t (&key)[kVec]) const {
+  // The same without a branch, for rows of kVec labels at least: near the end the row's last labels are read, and
+  // shift_end() puts them in their places.
+  __device__ __forceinline__ Piece load_ahead(int first) const {
+    Piece p;
+    p.scores = *(const Unaligned *)(scores + min(first, labels - kVec));
+    p.listed = 0;
+    if (bits) p.listed = bits[min(first, labels - 1) >> 5] >> (first & 31);
+    return p;
+  }
+  __device__ __forceinline__ void shift_end(int first, Piece &p) const {
+    if (first + kVec <= labels) return;
+    struct All { T v[kVec]; };
+    All e = __builtin_bit_cast(All, p.scores);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {   // (labels from the last kVec on: one place to the left per round)
+#pragma unroll
+      for (int i = 0; i + 1 < kVec; ++i) e.v[i] = first - (labels - kVec) > j ? e.v[i + 1] : e.v[i];
+    }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (first + j >= labels) e.v[j] = (T)-__builtin_inff();
+    p.scores = __builtin_bit_cast(Words, e);
+  }
+  // the scores themselves, fp32: NaN is -inf, -0 is 0, listed ones have the offset added
+  __device__ __forceinline__ void values(const Piece &p, float (&x)[kVec]) const {
     struct All { T v[kVec]; };
     const All e = __builtin_bit_cast(All, p.scores);
+    if (bits) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const float x = (float)e.v[j];
-      key[j] = score_key(p.listed >> j & 1 ? x + offset : x);
+      for (int j = 0; j < kVec; ++j) x[j] = (float)e.v[j] + (p.listed >> j & 1 ? offset : 0.0f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) x[j] = (float)e.v[j] + 0.0f;
     }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) x[j] = fmaxf(x[j], -__builtin_inff());
   }
 };
 
-// A workgroup of kBlock threads per row.  kHeld: the row is read once and kept as keys in LDS (every thread reads its own
+// A workgroup of kBlock threads per row.  kHeld: the row is read once and kept as fp32 in LDS (every thread reads its own
 // again); otherwise it is read again for each step.
 //
 // The kept labels are always a beginning of the order, so they are described by a key and a number of labels that have
@@ -147,11 +195,11 @@ template <typename T> struct Row {
 // down, and the bin where it passes the border is the next interval, narrowed to the keys that occur in it, until one
 // key is left.  All sums are of integers, so their order does not matter.
 template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
-  constexpr int kWaves = kBlock / 64, kVec = Row<T>::kVec, kAhead = 4, kMaxCells = kHeld ? 1 : 32;
+  constexpr int kWaves = kBlock / 64, kVec = kHeld ? 16 / sizeof(T) : 4, kMaxCells = kHeld ? 1 : 32;
   constexpr int kNear = !kHeld ? 8192 : kBlock == 1024 ? 512 : kList;
-  extern __shared__ uint4 held[];   // kHeld: the row's keys, by label
-  __shared__ uint64_t bins[kBlock];   // of a histogram; later the gathered labels: key << 32 | ~label (larger: earlier in the order)
-  // labels near the cut, unordered (key << 32 | ~label); or the weights of the gathered labels, in the order
+  extern __shared__ float4 held[];   // kHeld: the row, by label
+  __shared__ uint64_t bins[kBlock];   // of a histogram; later weights of listed labels
+  // labels near the cut, or all that may be kept: key << 32 | ~label (larger: earlier in the order), in no order
   __shared__ uint64_t near[kNear];
   __shared__ uint64_t cell_mass[kWaves * kMaxCells], wave_mass[kWaves];
   __shared__ uint32_t cell_ties[kWaves * kMaxCells], wave_a[kWaves], wave_b[kWaves], wave_c[kWaves];
@@ -172,56 +220,61 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   const int k = p.top_k ? p.top_k[r] : 0;
   const float top_p = p.top_p ? p.top_p[r] : 1.0f, min_p = p.min_p ? p.min_p[r] : 0.0f;
   float random = p.random[r];
-  Row<T> row{(const T *)p.scores + (int64_t)r * p.row_stride, nullptr, p.offsets[ch], N};
+  typedef Row<T, kVec> RowT;
+  RowT row{(const T *)p.scores + (int64_t)r * p.row_stride, nullptr, p.offsets[ch], N};
   if (row.offset != 0.0f) row.bits = p.bits + (int64_t)ch * p.words;
   const int turns = (N + kBlock * kVec - 1) / (kBlock * kVec);
   const int first = (wave * turns * 64 + lane) * kVec;   // of turn 0
+  float best = -__builtin_inff();
   if constexpr (kHeld) {
     for (int t = 0; t < turns; ++t) {
-      uint32_t key[kVec];
-      row.keys(row.load(first + t * 64 * kVec), key);
+      float x[kVec];
+      row.values(row.load(first + t * 64 * kVec), x);
+      for (int j = 0; j < kVec; ++j) best = fmaxf(best, x[j]);
 #pragma unroll
-      for (int q = 0; q < kVec / 4; ++q) held[(first + t * 64 * kVec) / 4 + q] = make_uint4(key[4 * q], key[4 * q + 1], key[4 * q + 2], key[4 * q + 3]);
+      for (int q = 0; q < kVec / 4; ++q) held[(first + t * 64 * kVec) / 4 + q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
     }
   }
-  // the thread's keys of turn t
-  auto load_turn = [&](int t, uint32_t (&key)[kVec]) {
+  const int whole_turns = (int)((unsigned)N / (64u * kVec)) - __builtin_amdgcn_readfirstlane(wave) * turns;   // of this wave
+  // the thread's scores of turn t
+  auto load_turn = [&](int t, float (&x)[kVec]) __attribute__((always_inline)) {
     if constexpr (kHeld) {
 #pragma unroll
       for (int q = 0; q < kVec / 4; ++q) {
-        const uint4 v = held[(first + t * 64 * kVec) / 4 + q];
-        key[4 * q] = v.x; key[4 * q + 1] = v.y; key[4 * q + 2] = v.z; key[4 * q + 3] = v.w;
+        const float4 v = held[(first + t * 64 * kVec) / 4 + q];
+        x[4 * q] = v.x; x[4 * q + 1] = v.y; x[4 * q + 2] = v.z; x[4 * q + 3] = v.w;
       }
     } else {
-      row.keys(row.load(first + t * 64 * kVec), key);
+      row.values(row.load(first + t * 64 * kVec), x);
     }
   };
-  // f(turn, keys) for all of the thread's turns; rows that are read again: kAhead turns on their way
-  auto each_turn = [&](auto f) {
+  // f(turn, scores) for all of the thread's turns; rows that are read again: two turns on their way
+  auto each_turn = [&](auto f) __attribute__((always_inline)) {
     if constexpr (kHeld) {
 #pragma unroll 1
       for (int t = 0; t < turns; ++t) {
-        uint32_t key[kVec];
-        load_turn(t, key);
-        f(t, key);
+        float x[kVec];
+        load_turn(t, x);
+        f(t, x);
       }
     } else {
-      typename Row<T>::Piece next[kAhead];
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a) next[a] = row.load(a < turns ? first + a * 64 * kVec : N);
+      typename RowT::Piece even = row.load_ahead(first), odd = row.load_ahead(first + 64 * kVec);
+      auto one = [&](int t, typename RowT::Piece &p) __attribute__((always_inline)) {
+        float x[kVec];
+        if (t >= whole_turns) row.shift_end(first + t * 64 * kVec, p);
+        row.values(p, x);
+        p = row.load_ahead(first + (t + 2) * 64 * kVec);
+        f(t, x);
+      };
 #pragma unroll 1
-      for (int t = 0; t < turns; ++t) {
-        uint32_t key[kVec];
-        row.keys(next[0], key);
-#pragma unroll
-        for (int a = 1; a < kAhead; ++a) next[a - 1] = next[a];
-        next[kAhead - 1] = row.load(t + kAhead < turns ? first + (t + kAhead) * 64 * kVec : N);
-        f(t, key);
+      for (int t = 0; t < turns; t += 2) {
+        one(t, even);
+        if (t + 1 < turns) one(t + 1, odd);
       }
     }
   };
   // the largest and the smallest of what the waves give, to all
-  auto block_range = [&](uint32_t hi, uint32_t lo, uint32_t *hi_out, uint32_t *lo_out) {
+  auto block_range = [&](uint32_t hi, uint32_t lo, uint32_t *hi_out, uint32_t *lo_out) __attribute__((always_inline)) {
     hi = wave_max(hi);
     lo = wave_min(lo);
     __syncthreads();
@@ -232,98 +285,62 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     for (int w = 1; w < kWaves; ++w) { hi = max32(hi, wave_a[w]); lo = min32(lo, wave_b[w]); }
     *hi_out = hi; *lo_out = lo;
   };
-  // the lowest label of those for which f(key) holds, to all; N if none
-  auto lowest_label = [&](auto f) {
+  // the lowest label of those for which f(score) holds, to all; N if none
+  auto lowest_label = [&](auto f) __attribute__((always_inline)) {
     uint32_t at = (uint32_t)N;
-    each_turn([&](int t, const uint32_t (&key)[kVec]) {
+    each_turn([&](int t, const float (&x)[kVec]) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = kVec - 1; j >= 0; --j)
-        if (f(key[j])) at = min32(at, (uint32_t)(first + t * 64 * kVec + j));
+        if (f(x[j])) at = min32(at, (uint32_t)(first + t * 64 * kVec + j));
     });
     uint32_t hi, lo;
     block_range(0, at, &hi, &lo);
     return (int)lo;
   };
-  uint32_t best_key, last_key;
-  {
-    uint32_t hi = 0, lo = 0xFFFFFFFFu;
-    each_turn([&](int, const uint32_t (&key)[kVec]) {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) { hi = max32(hi, key[j]); lo = min32(lo, key[j] - 1u); }   // (masked: 0 - 1 is the largest)
-    });
-    block_range(hi, lo, &best_key, &last_key);
-    last_key += 1u;
-  }
-  if (best_key == 0) {
-    if (tid == 0) write(-1, -__builtin_inff(), 0);
+  if constexpr (!kHeld) each_turn([&](int, const float (&x)[kVec]) __attribute__((always_inline)) {
+    for (int j = 0; j < kVec; ++j) best = fmaxf(best, x[j]);
+  });
+  uint32_t best_key, unused;
+  block_range(score_key(best), 0, &best_key, &unused);
+  best = key_score(best_key);
+  if (best == -__builtin_inff()) {
+    if (tid == 0) write(-1, best, 0);
     return;
   }
   if (!(temperature > 0.0f)) {
-    const int label = lowest_label([&](uint32_t key) { return key == best_key; });
+    const int label = lowest_label([&](float x) __attribute__((always_inline)) { return x == best; });
     if (tid == 0) write(label, 0.0f, 1);
     return;
   }
-  const float best = key_score(best_key);
-  if (best == __builtin_inff()) last_key = best_key;   // (scores of +inf leave the others no mass)
-  const Weigher wt{(double)best, 1.0 / (double)temperature, 1.4426950408889634 / (double)temperature, (double)p.unit_bits};
+  const uint32_t last_key = best == __builtin_inff() ? best_key : kLowestKey;   // (scores of +inf leave the others no mass)
+  const Weigher wt{(double)fminf(best, kLargest), 1.0 / (double)temperature, 1.4426950408889634 / (double)temperature, (double)p.unit_bits};
   uint32_t cut = last_key, ties = kAllTies;
 
-  // labels with keys from `floor` on, gathered by their wave and lane, for n of them at most kList (n is exact)
-  auto gather = [&](uint32_t floor) {
-    uint32_t n = 0;
-    each_turn([&](int, const uint32_t (&key)[kVec]) {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) n += key[j] >= floor;
-    });
-    n = wave_sum(n);
-    __syncthreads();
-    if (lane == 0) wave_a[wave] = n;
-    __syncthreads();
-    uint32_t at = 0;
-    for (int w = 0; w < wave; ++w) at += wave_a[w];
-    each_turn([&](int t, const uint32_t (&key)[kVec]) {
-      n = 0;
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) n += key[j] >= floor;
-      if (!__ballot(n != 0)) return;
-      const uint32_t upto = wave_scan(n);
-      uint32_t to = at + upto - n;
-      at += last_lane(upto);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        if (key[j] >= floor) bins[to++] = (uint64_t)key[j] << 32 | (uint32_t)~(first + t * 64 * kVec + j);
-    });
-    __syncthreads();
+  // f(score) for all of the row's labels, and for the labels in `near`
+  auto each_score = [&](auto f) __attribute__((always_inline)) {
+    each_turn([&](int, const float (&x)[kVec]) __attribute__((always_inline)) { each_of<kVec>([&](int j) __attribute__((always_inline)) { f(x[j]); }); });
   };
-  // f(key) for all of the row's labels, and for the labels in `near`
-  auto each_key = [&](auto f) {
-    each_turn([&](int, const uint32_t (&key)[kVec]) {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        f(key[j]);
-        if (j & 1) __builtin_amdgcn_sched_barrier(0);
-      }
-    });
-  };
-  auto each_near = [&](auto f) {
-    for (uint32_t i = tid; i < n_near; i += kBlock) f((uint32_t)(near[i] >> 32));
+  auto each_near = [&](auto f) __attribute__((always_inline)) {
+    for (uint32_t i = tid; i < n_near; i += kBlock) f(key_score((uint32_t)(near[i] >> 32)));
   };
   // Keys from lo to hi, in which the running count or mass, from best_key down, reaches `want`; `before` is the sum over
   // larger keys, `from_lo` (counts only) the number of labels with keys from lo on.
   struct Interval { uint32_t lo, hi; uint64_t before; double want; uint32_t from_lo; };
-  // One step: bins of the interval, and the one in which the sum passes `want` becomes the interval.
-  auto narrow = [&](auto by_mass, auto each, Interval &v, auto want_of) {
+  // One step: bins over the keys from hi down to `end` (the last bin takes those down to lo as well), and the one in which
+  // the sum passes `want` becomes the interval.
+  auto narrow = [&](auto by_mass, auto each, Interval &v, uint32_t end, auto want_of) __attribute__((always_inline)) {
     constexpr bool kMass = decltype(by_mass)::value;
-    const int width = 32 - __clz((int)((v.hi - v.lo) | 1u)), log2 = kBlock == 1024 ? 10 : 8;
+    const int width = 32 - __clz((int)((v.hi - max32(end, v.lo)) | 1u)), log2 = kBlock == 1024 ? 10 : 8;
     const int shift = width > log2 ? width - log2 : 0;
     __syncthreads();
     bins[tid] = 0;
     __syncthreads();
-    each([&](uint32_t key) {
-      if (key >= v.lo && key <= v.hi) {
-        const uint32_t b = (v.hi - key) >> shift;
+    const float lo = key_score(v.lo), hi = key_score(v.hi);
+    each([&](float x) __attribute__((always_inline)) {
+      if (x >= lo && x <= hi) {
+        const uint32_t b = min32((v.hi - score_key(x)) >> shift, kBlock - 1);
         if constexpr (kMass) {
-          const uint64_t u = wt.units(key);
+          const uint64_t u = wt.units(x);
           if (u) atomicAdd((unsigned long long *)&bins[b], (unsigned long long)u);
         } else {
           atomicAdd((uint32_t *)&bins[b], 1u);
@@ -350,16 +367,17 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     }
     __syncthreads();
     v.before = pick_before;
-    v.hi -= pick_bin << shift;
-    if ((v.hi - v.lo) >> shift) v.lo = v.hi - (1u << shift) + 1u;
     v.from_lo = pick_count;
+    v.hi -= pick_bin << shift;
+    if (pick_bin < kBlock - 1 && (v.hi - v.lo) >> shift) v.lo = v.hi - (1u << shift) + 1u;
   };
   auto as_before = [](uint64_t, double want) { return want; };
   // ... and down to the keys that occur in it
-  auto tighten = [&](auto each, Interval &v) {
+  auto tighten = [&](auto each, Interval &v) __attribute__((always_inline)) {
     uint32_t top = 0, low = 0xFFFFFFFFu;
-    each([&](uint32_t key) {
-      if (key >= v.lo && key <= v.hi) { top = max32(top, key); low = min32(low, key); }
+    const float lo = key_score(v.lo), hi = key_score(v.hi);
+    each([&](float x) __attribute__((always_inline)) {
+      if (x >= lo && x <= hi) { top = max32(top, score_key(x)); low = min32(low, score_key(x)); }
     });
     block_range(top, low, &v.hi, &v.lo);
   };
@@ -368,29 +386,33 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   const int cells = (turns + cell_turns - 1) / cell_turns;   // per wave
   uint64_t mass = 0;
   uint32_t at_cut = 0;
-  auto end_cell = [&](int cell) {
+  auto end_cell = [&](int cell) __attribute__((always_inline)) {
     mass = wave_sum(mass);
     at_cut = wave_sum(at_cut);
     if (lane == 0) { cell_mass[wave * cells + cell] = mass; cell_ties[wave * cells + cell] = at_cut; }
     mass = 0; at_cut = 0;
   };
-  auto is_cell_end = [&](int t) { return t > 0 && t % cell_turns == 0 && t < turns; };
+  int cell_left;   // turns until the present cell ends
+  auto next_turn = [&](int t) __attribute__((always_inline)) {
+    if (cell_left == 0) { end_cell(t / cell_turns - 1); cell_left = cell_turns; }
+    --cell_left;
+  };
   // One pass that notes the labels with keys from lo to hi in `near` and sums those above per cell (wave_c: their number).
   // False if there are more than fit.
-  auto collect = [&](uint32_t lo, uint32_t hi) {
+  auto collect = [&](uint32_t lo_key, uint32_t hi_key) __attribute__((always_inline)) {
+    const float lo = key_score(lo_key), hi = key_score(hi_key);
     __syncthreads();
     if (tid == 0) n_near = 0;
     __syncthreads();
     uint32_t above = 0;
-    each_turn([&](int t, const uint32_t (&key)[kVec]) {
-      if (is_cell_end(t)) end_cell(t / cell_turns - 1);
+    cell_left = cell_turns;
+    each_turn([&](int t, const float (&x)[kVec]) __attribute__((always_inline)) {
+      next_turn(t);
       uint32_t n = 0;
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        if (key[j] > hi) { mass += wt.units(key[j]); ++above; }
-        n += key[j] >= lo && key[j] <= hi;
-        if (j & 1) __builtin_amdgcn_sched_barrier(0);
-      }
+      each_of<kVec>([&](int j) __attribute__((always_inline)) {
+        if (x[j] > hi) { mass += wt.units(x[j]); ++above; }
+        n += x[j] >= lo && x[j] <= hi;
+      });
       if (!__ballot(n != 0)) return;
       const uint32_t upto = wave_scan(n), all = last_lane(upto);
       uint32_t at = 0;
@@ -398,8 +420,8 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at) + upto - n;
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        if (key[j] >= lo && key[j] <= hi) {
-          if (at < (uint32_t)kNear) near[at] = (uint64_t)key[j] << 32 | (uint32_t)~(first + t * 64 * kVec + j);
+        if (x[j] >= lo && x[j] <= hi) {
+          if (at < (uint32_t)kNear) near[at] = (uint64_t)score_key(x[j]) << 32 | (uint32_t)~(first + t * 64 * kVec + j);
           ++at;
         }
     });
@@ -409,59 +431,80 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     __syncthreads();
     return n_near <= (uint32_t)kNear;
   };
-  // Finds cut and ties from `v`, an interval of more than one step's narrowing; kMass: ties follow from the mass.
-  auto settle = [&](auto by_mass, Interval &v) {
+  // Finds cut and ties: the first `want` labels or the mass `want` (want_of: from the sum of all) of those with keys from
+  // v.lo on.  list_all: stops as soon as no more than kList labels have keys from v.lo on (counts only; true then).
+  // *listed: labels above this key are in the cells of collect(), those down to cut in `near`; 0: they are not.
+  auto search = [&](auto by_mass, Interval &v, auto want_of, bool list_all, uint32_t *listed) __attribute__((always_inline)) {
     constexpr bool kMass = decltype(by_mass)::value;
-    bool listed = false;
-    while (v.lo != v.hi && !listed) {
-      listed = collect(v.lo, v.hi);
-      if (!listed) {
-        tighten(each_key, v);
-        if (v.lo != v.hi) narrow(by_mass, each_key, v, as_before);
-      }
+    // bins reach down to weights of 2^-46 (or, for counts, to scores 40 below the best): beyond, the search begins anew
+    const double reach = kMass ? 32.0 * (double)temperature : 40.0;
+    uint32_t end = score_key((float)fmax((double)fminf(best, kLargest) - reach, -(double)kLargest));
+    *listed = 0;
+    for (bool begun = false;; begun = true) {
+      narrow(by_mass, each_score, v, end, [&](uint64_t all, double want) __attribute__((always_inline)) { return begun ? want : want_of(all); });
+      if (!kMass && list_all && v.from_lo <= (uint32_t)kList) return true;
+      if (v.lo == v.hi) break;
+      if (!list_all && collect(v.lo, v.hi)) { *listed = v.hi; break; }
+      tighten(each_score, v);
+      if (v.lo == v.hi) break;
+      end = v.lo;
     }
-    const uint32_t top = v.hi;
     while (v.lo != v.hi) {
       tighten(each_near, v);
-      if (v.lo != v.hi) narrow(by_mass, each_near, v, as_before);
+      if (v.lo != v.hi) narrow(by_mass, each_near, v, v.lo, as_before);
     }
     uint32_t t = kAllTies;
-    const uint64_t w = wt.units(v.hi);
-    if (!kMass) {
+    if constexpr (!kMass) {
       t = (uint32_t)(v.want - (double)v.before);
-    } else if (w > 0) {
+    } else {
       // labels j = 0, 1, ... with this key are kept while before + j * (their weight) < want
-      const double j = ceil((v.want - (double)v.before) / (double)w);
+      const uint64_t w = wt.units(key_score(v.hi));
+      const double j = w > 0 ? ceil((v.want - (double)v.before) / (double)w) : 4e9;
       t = j < 1.0 ? 1u : j < 4e9 ? (uint32_t)j : kAllTies;
     }
     if (v.hi > cut) { cut = v.hi; ties = t; }
     else ties = min32(ties, t);
-    return listed ? top : 0u;   // labels above this key are in the cells, those down to cut in `near`
+    return false;
   };
-  auto enough = [&](uint32_t key, double least) { return exp(wt.log_weight(key)) >= least; };   // min_p's test
-  // The rest on n gathered labels: the first `most` of the order, of these those with less than `want` before them (share
-  // >= 0: want is this share of the mass of the first `most`), then min_p and the choice.
-  auto finish_list = [&](int n, uint32_t most, double share, double want) {
-    const uint64_t me = tid < n ? bins[tid] : 0;
-    const uint32_t key = (uint32_t)(me >> 32);
-    uint32_t rank = 0;
-    uint64_t w = 0;
-    if (tid < n) {
+  auto enough = [&](float x, double least) __attribute__((always_inline)) { return exp(wt.log_weight(x)) >= least; };   // min_p's test
+  // The rest where all labels that may be kept, n of them, are in `near`: the first `most` of the order, of these those
+  // with less than `want` before them (share >= 0: want is this share of the mass of the first `most`), then min_p and the
+  // choice.  A thread has one label; its places in the order and by label are found by comparing it with all others.
+  auto finish_list = [&](int n, uint32_t most, double share, double want) __attribute__((always_inline)) {
+    const bool have = tid < n, in_list = tid < kList;   // (waves beyond the list only keep step)
+    const uint64_t me = have ? near[tid] : 0;
+    const float score = key_score((uint32_t)(me >> 32));
+    uint32_t rank = 0, place = 0;
+    uint64_t w = 0, v = 0, upto = 0;
+    if (have) {
 #pragma unroll 4
-      for (int j = 0; j < n; ++j) rank += bins[j] > me;
-      w = wt.units(key);
-      near[rank] = w;
+      for (int j = 0; j < n; ++j) {
+        const uint64_t other = near[j];
+        rank += other > me;
+        place += (uint32_t)other > (uint32_t)me;   // (~label: larger is lower)
+      }
+      w = wt.units(score);
+      bins[rank] = w;
     }
-    __syncthreads();
-    const bool in_list = tid < kList;   // (waves beyond the list only keep step)
-    uint64_t v = in_list && tid < n ? near[tid] : 0, upto = 0;
-    if (in_list) {
-      upto = wave_scan(v);
-      if (lane == 63) wave_mass[wave] = upto;
-    }
-    __syncthreads();
-    if (in_list)
-      for (int i = 0; i < wave; ++i) upto += wave_mass[i];
+    // sum up to this thread's entry of bins, over the first n; *all: of all of them
+    auto scan_bins = [&](uint64_t *all) __attribute__((always_inline)) {
+      __syncthreads();
+      v = have ? bins[tid] : 0;
+      if (in_list) {
+        upto = wave_scan(v);
+        if (lane == 63) wave_mass[wave] = upto;
+      }
+      __syncthreads();
+      uint64_t sum = 0;
+#pragma unroll
+      for (int i = 0; i < kList / 64; ++i) {
+        if (i < wave) upto += wave_mass[i];
+        sum += wave_mass[i];
+      }
+      *all = sum;
+    };
+    uint64_t total;
+    scan_bins(&total);
     most = min32(most, (uint32_t)n);
     if (share >= 0.0) {
       if (tid == (int)most - 1) pick_before = upto;
@@ -470,9 +513,8 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     }
     // three beginnings of the order: the shortest counts
     const double least = min_p > 0.0f ? (double)fminf(min_p, 1.0f) : 0.0;
-    const uint64_t by_mass = __ballot(tid < n && (tid == 0 || (double)(upto - v) < want));
-    const uint64_t by_min = __ballot(tid < n && (least == 0.0 || enough(key, least)));
-    __syncthreads();
+    const uint64_t by_mass = __ballot(have && (tid == 0 || (double)(upto - v) < want));
+    const uint64_t by_min = __ballot(have && (least == 0.0 || enough(score, least)));
     if (in_list && lane == 0) { wave_a[wave] = __popcll(by_mass); wave_b[wave] = __popcll(by_min); }
     __syncthreads();
     uint32_t n_mass = 0, n_min = 0;
@@ -480,54 +522,32 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     for (int i = 0; i < kList / 64; ++i) { n_mass += wave_a[i]; n_min += wave_b[i]; }
     const uint32_t kept = min32(most, min32(n_mass, n_min));
     // by label
-    const bool mine = tid < n && rank < kept;
-    v = mine ? w : 0;
-    if (in_list) {
-      upto = wave_scan(v);
-      if (lane == 63) wave_mass[wave] = upto;
-    }
-    __syncthreads();
-    uint64_t total = 0;
-    for (int i = 0; i < kList / 64; ++i) {
-      if (i < wave) upto += wave_mass[i];
-      total += wave_mass[i];
-    }
-    bool chosen;
+    const bool mine = have && rank < kept;
+    if (have) bins[place] = mine ? w : 0;
+    if (tid == 0) pick_bin = kAllTies;
+    scan_bins(&total);
     if (!(random > 0.0f)) {
-      const uint64_t some = __ballot(mine && wt.log_weight(key) > -745.13);   // (its weight is not zero in 64 bits)
-      __syncthreads();
-      if (in_list && lane == 0) wave_a[wave] = some ? __ffsll((unsigned long long)some) - 1 : 64;
-      __syncthreads();
-      int at = 0;
-      while (wave_a[at >> 6] == 64) at += 64;   // (the best label has weight)
-      chosen = tid == at + (int)wave_a[at >> 6];
+      if (mine && wt.log_weight(score) > -745.13) atomicMin(&pick_bin, place);   // (its weight is not zero in 64 bits)
     } else {
       uint64_t target = (uint64_t)((double)random * (double)total);
       if (random >= 1.0f || target >= total) target = total - 1;
-      chosen = in_list && upto > target && upto - v <= target;
+      if (have && upto > target && upto - v <= target) pick_bin = (uint32_t)tid;
     }
-    if (chosen)
-      write((int)~(uint32_t)me, (float)(wt.log_weight(key) - log((double)total * ldexp(1.0, -p.unit_bits))), (int)kept);
+    __syncthreads();
+    if (mine && place == pick_bin)
+      write((int)~(uint32_t)me, (float)(wt.log_weight(score) - log((double)total * ldexp(1.0, -p.unit_bits))), (int)kept);
   };
   const bool by_count = k > 0 && k < N, by_share = top_p < 1.0f;
   uint32_t listed_from = 0;   // not 0: collect()'s sums are of larger keys, and the rest of the kept labels is in `near`
   if (by_count) {
     Interval v{last_key, best_key, 0, 0.0, kAllTies};
-    bool cuts = true;
-    narrow(std::false_type(), each_key, v, [&](uint64_t all, double) {
-      cuts = (uint64_t)k < all;
-      return cuts ? (double)k : (double)all;   // (fewer labels than that: nothing is cut)
-    });
-    while (v.from_lo > (uint32_t)kList && k <= kList && v.lo != v.hi) {
-      tighten(each_key, v);
-      narrow(std::false_type(), each_key, v, as_before);
-    }
-    if (v.from_lo <= (uint32_t)kList) {
-      gather(v.lo);
+    uint64_t valid = 0;   // (no more labels than top_k: nothing is cut)
+    if (search(std::false_type(), v, [&](uint64_t all) __attribute__((always_inline)) { valid = all; return (double)min((uint64_t)k, all); }, k <= kList, &listed_from)) {
+      collect(v.lo, best_key);
       finish_list((int)v.from_lo, (uint32_t)k, by_share ? (double)max(top_p, 0.0f) : -1.0, __builtin_inf());
       return;
     }
-    if (cuts) listed_from = settle(std::false_type(), v);
+    if (valid <= (uint64_t)k) ties = kAllTies;
   }
   if (top_p <= 0.0f) {
     cut = best_key; ties = 1; listed_from = 0;
@@ -536,7 +556,8 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     uint64_t left_out = 0;
     if (ties != kAllTies) {
       uint32_t n = 0;
-      each_key([&](uint32_t key) { n += key == cut; });
+      const float x_cut = key_score(cut);
+      each_score([&](float x) __attribute__((always_inline)) { n += x == x_cut; });
       n = wave_sum(n);
       __syncthreads();
       if (lane == 0) wave_a[wave] = n;
@@ -544,26 +565,25 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       n = 0;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) n += wave_a[w];
-      left_out = (uint64_t)(n - ties) * wt.units(cut);
+      left_out = (uint64_t)(n - ties) * wt.units(x_cut);
     }
     Interval v{cut, best_key, 0, 0.0, kAllTies};
-    narrow(std::true_type(), each_key, v, [&](uint64_t all, double) { return (double)top_p * (double)(all - left_out); });
-    listed_from = settle(std::true_type(), v);
+    search(std::true_type(), v, [&](uint64_t all) __attribute__((always_inline)) { return (double)top_p * (double)(all - left_out); }, false, &listed_from);
   }
   if (min_p > 0.0f) {
     // the smallest key with exp(log_weight) >= min_p: guessed, and found among its neighbours, 64 at a time
     const double least = (double)fminf(min_p, 1.0f);
-    const uint32_t guess = score_key((float)(wt.best + (double)temperature * log(least)));
+    const uint32_t guess = score_key((float)fmax(wt.best + (double)temperature * log(least), -(double)kLargest));
     uint32_t from = guess > last_key + 32u ? guess - 32u : last_key;   // lane 0's key
     if (from > best_key) from = best_key;
-    uint64_t yes = __ballot(from + lane <= best_key && enough(min32(from + lane, best_key), least));
+    uint64_t yes = __ballot(from + lane <= best_key && enough(key_score(min32(from + lane, best_key)), least));
     if (from + 63u >= best_key) yes |= 1ull << (best_key - from);   // (the best always is)
     if (!yes || (yes & 1ull && from > last_key)) {
       // not there: the whole interval, a 64th of what is left at a time; lo stays a key that is not enough or last_key
       uint32_t lo = last_key, hi = best_key;   // hi is enough
       while (hi > lo) {
         const uint32_t step = (hi - lo) / 64u + 1u, key = lo + (uint64_t)lane * step < hi ? lo + (uint32_t)lane * step : hi;
-        const uint64_t ok = __ballot(key == hi || enough(key, least));
+        const uint64_t ok = __ballot(key == hi || enough(key_score(key), least));
         const int l = __ffsll((unsigned long long)ok) - 1;
         const uint32_t at = __shfl(key, l), under = l > 0 ? __shfl(key, l - 1) + 1u : at;
         hi = at;
@@ -579,26 +599,14 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     }
     if (!by_count && !by_share) {
       // few labels are left, as a rule
-      uint32_t n = 0;
-      each_turn([&](int, const uint32_t (&key)[kVec]) {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) n += key[j] >= cut;
-      });
-      n = wave_sum(n);
-      __syncthreads();
-      if (lane == 0) wave_c[wave] = n;
-      __syncthreads();
-      n = 0;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) n += wave_c[w];
-      if (n <= kList) {
-        gather(cut);
-        finish_list((int)n, kAllTies, -1.0, __builtin_inf());
+      if (collect(cut, best_key) && n_near <= (uint32_t)kList) {
+        finish_list((int)n_near, kAllTies, -1.0, __builtin_inf());
         return;
       }
     }
   }
-  const uint64_t w_cut = wt.units(cut);
+  const float x_cut = key_score(cut);
+  const uint64_t w_cut = wt.units(x_cut);
   if (listed_from) {
     // the cells lack the labels in `near`
     const uint32_t n = n_near;
@@ -607,7 +615,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
       const uint32_t key = (uint32_t)(near[i] >> 32), g = ~(uint32_t)near[i] / (64u * kVec);
       const uint32_t cell = g / (uint32_t)turns * cells + g % (uint32_t)turns / cell_turns;
       if (key > cut) {
-        atomicAdd((unsigned long long *)&cell_mass[cell], (unsigned long long)wt.units(key));
+        atomicAdd((unsigned long long *)&cell_mass[cell], (unsigned long long)wt.units(key_score(key)));
         atomicAdd(&wave_c[0], 1u);
       } else if (key == cut) {
         atomicAdd(&cell_ties[cell], 1u);
@@ -616,14 +624,13 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   } else {
     uint32_t above = 0;
     __syncthreads();
-    each_turn([&](int t, const uint32_t (&key)[kVec]) {
-      if (is_cell_end(t)) end_cell(t / cell_turns - 1);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        if (key[j] > cut) { mass += wt.units(key[j]); ++above; }
-        at_cut += key[j] == cut;
-        if (j & 1) __builtin_amdgcn_sched_barrier(0);
-      }
+    cell_left = cell_turns;
+    each_turn([&](int t, const float (&x)[kVec]) __attribute__((always_inline)) {
+      next_turn(t);
+      each_of<kVec>([&](int j) __attribute__((always_inline)) {
+        if (x[j] > x_cut) { mass += wt.units(x[j]); ++above; }
+        at_cut += x[j] == x_cut;
+      });
     });
     end_cell(cells - 1);
     above = wave_sum(above);
@@ -640,17 +647,16 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   uint32_t kept = (uint32_t)kept_ties;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) kept += wave_c[w];
-  auto answer = [&](int label, uint32_t key) {
-    write(label, (float)(wt.log_weight(key) - log((double)total * ldexp(1.0, -p.unit_bits))), (int)kept);
+  auto answer = [&](int label, float x) __attribute__((always_inline)) {
+    write(label, (float)(wt.log_weight(x) - log((double)total * ldexp(1.0, -p.unit_bits))), (int)kept);
   };
   if (!(random > 0.0f)) {
     // the first kept label whose weight is not zero in 64 bits
-    auto some = [&](uint32_t key) { return key >= cut && wt.log_weight(key) > -745.13; };
-    const int label = lowest_label(some);
-    each_turn([&](int t, const uint32_t (&key)[kVec]) {
+    const int label = lowest_label([&](float x) __attribute__((always_inline)) { return x >= x_cut && wt.log_weight(x) > -745.13; });
+    each_turn([&](int t, const float (&x)[kVec]) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        if (first + t * 64 * kVec + j == label) answer(label, key[j]);
+        if (first + t * 64 * kVec + j == label) answer(label, x[j]);
     });
     return;
   }
@@ -672,44 +678,33 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   if (wave != cell / cells) return;
   const int t0 = cell % cells * cell_turns, t1 = min(t0 + cell_turns, turns);
   bool found = false;
-  auto look = [&](int t, const uint32_t (&key)[kVec]) {   // (all lanes of the wave)
-    if (found) return;
+#pragma unroll 1
+  for (int t = t0; t < t1 && !found; ++t) {   // (all lanes of the wave)
+    float x[kVec];
+    load_turn(t, x);
     uint64_t m = 0;
     uint32_t n = 0;
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      if (key[j] > cut) m += wt.units(key[j]);
-      n += key[j] == cut;
-    }
+    each_of<kVec>([&](int j) __attribute__((always_inline)) {
+      if (x[j] > x_cut) m += wt.units(x[j]);
+      n += x[j] == x_cut;
+    });
     const uint64_t m_upto = wave_scan(m);
     const uint32_t n_upto = wave_scan(n);
     const uint64_t upto = run + m_upto + (uint64_t)kept_of(rank, n_upto) * w_cut;
     const uint64_t passed = __ballot(upto > target);
-    if (passed) {
-      found = true;
-      if (lane == __ffsll((unsigned long long)passed) - 1) {
-        uint32_t before = rank + n_upto - n;
-        uint64_t sum = run + m_upto - m + (uint64_t)kept_of(rank, n_upto - n) * w_cut;
-        bool done = false;
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-          if (done || key[j] < cut) continue;
-          if (key[j] == cut && before++ >= ties) continue;
-          sum += wt.units(key[j]);
-          if (sum > target) { done = true; answer(first + t * 64 * kVec + j, key[j]); }
-        }
-      }
-      return;
+    found = passed != 0;
+    if (found && lane == __ffsll((unsigned long long)passed) - 1) {
+      uint32_t before = rank + n_upto - n;
+      uint64_t sum = run + m_upto - m + (uint64_t)kept_of(rank, n_upto - n) * w_cut;
+      bool done = false;
+      each_of<kVec>([&](int j) __attribute__((always_inline)) {
+        if (done || x[j] < x_cut || (x[j] == x_cut && before++ >= ties)) return;
+        sum += wt.units(x[j]);
+        if (sum > target) { done = true; answer(first + t * 64 * kVec + j, x[j]); }
+      });
     }
-    run = last_lane(upto);
-    // (run counts the kept ties of this turn already; rank moves on for the next)
+    run = last_lane(upto);   // (with the kept ties of this turn)
     rank += last_lane(n_upto);
-  };
-#pragma unroll 1
-  for (int t = t0; t < t1; ++t) {
-    uint32_t key[kVec];
-    load_turn(t, key);
-    look(t, key);
   }
 }
 
@@ -746,7 +741,7 @@ constexpr int32_t kUpload = 1 << 15;   // entries of 8 bytes per upload slot
 constexpr size_t kHeldBytes = 144 * 1024;   // of LDS for a row's keys (with the kernel's own 9 KB: within 160 KB)
 
 template <typename T, int kBlock> size_t held_bytes(int num_labels) {   // whole turns
-  const size_t turn = (size_t)kBlock * cbd::Row<T>::kVec;
+  const size_t turn = (size_t)kBlock * (16 / sizeof(T));
   return ((size_t)num_labels + turn - 1) / turn * turn * sizeof(uint32_t);
 }
 
