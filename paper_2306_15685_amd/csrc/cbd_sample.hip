@@ -27,6 +27,7 @@ struct SampleParams {
   float *logprobs;
   int32_t num_labels, num_channels, words;   // words: 32-bit words of a channel's bits
   int32_t unit_bits;         // weights are summed in units of 2^-unit_bits
+  double series[9];          // ln(2)^k / k!, k = 9 .. 1 (arguments: they stay in scalar registers)
 };
 
 constexpr int kThreads = 256;   // of the kernels that set lists
@@ -43,16 +44,10 @@ __device__ __forceinline__ uint32_t score_key(float x) {
 __device__ __forceinline__ float key_score(uint32_t k) { return __uint_as_float(k ^ (~(uint32_t)((int32_t)k >> 31) | 0x80000000u)); }
 constexpr uint32_t kLowestKey = 0x00800000u;   // of the smallest finite score
 
-// a * b + c, c in scalar registers
-__device__ __forceinline__ double fma_const(double a, double b, double c) {
-  double r;
-  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
-  return r;
-}
-
 // Weights as integers: exp((x - best) / temperature) in units of 2^-unit_bits, with relative error below 2^-36.
 struct Weigher {
   double best, inv_t, slope, bits;   // slope = log2(e) / temperature
+  const double *series;              // ln(2)^k / k!, k = 9 .. 1
   // x - best, exact; scores of +inf (the best is one then) count as the largest finite number
   __device__ __forceinline__ double distance(float x) const { return (double)fminf(x, kLargest) - best; }
   __device__ __forceinline__ double log_weight(float x) const { return distance(x) * inv_t; }
@@ -63,14 +58,9 @@ struct Weigher {
   __device__ __forceinline__ uint64_t units(float x) const {
     constexpr double kMagic = 6755399441055744.0;
     const double y = fmax(fma(distance(x), slope, bits), -4.0), shifted = y + kMagic, f = y - (shifted - kMagic);
-    double e = fma_const(f, 1.0178086009239699e-07, 1.3215486790144307e-06);   // ln(2)^k / k!
-    e = fma_const(e, f, 1.5252733804059840e-05);
-    e = fma_const(e, f, 1.5403530393381608e-04);
-    e = fma_const(e, f, 1.3333558146428443e-03);
-    e = fma_const(e, f, 9.6181291076284770e-03);
-    e = fma_const(e, f, 5.5504108664821580e-02);
-    e = fma_const(e, f, 2.4022650695910072e-01);
-    e = fma_const(e, f, 6.9314718055994530e-01);
+    double e = fma(series[0], f, series[1]);
+#pragma unroll
+    for (int k = 2; k < 9; ++k) e = fma(e, f, series[k]);
     e = fma(e, f, 1.0);
     const uint32_t n = (uint32_t)__double_as_longlong(shifted);
     e = __hiloint2double(__double2hiint(e) + (int)(n << 20), __double2loint(e));
@@ -195,7 +185,7 @@ template <typename T, int kVec> struct Row {
 // down, and the bin where it passes the border is the next interval, narrowed to the keys that occur in it, until one
 // key is left.  All sums are of integers, so their order does not matter.
 template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
-  constexpr int kWaves = kBlock / 64, kVec = kHeld ? 16 / sizeof(T) : 4, kMaxCells = kHeld ? 1 : 32;
+  constexpr int kWaves = kBlock / 64, kVec = kHeld ? 16 / sizeof(T) : 4, kMaxCells = kHeld ? 1 : 16;
   constexpr int kNear = !kHeld ? 8192 : kBlock == 1024 ? 512 : kList;
   extern __shared__ float4 held[];   // kHeld: the row, by label
   __shared__ uint64_t bins[kBlock];   // of a histogram; later weights of listed labels
@@ -313,7 +303,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     return;
   }
   const uint32_t last_key = best == __builtin_inff() ? best_key : kLowestKey;   // (scores of +inf leave the others no mass)
-  const Weigher wt{(double)fminf(best, kLargest), 1.0 / (double)temperature, 1.4426950408889634 / (double)temperature, (double)p.unit_bits};
+  const Weigher wt{(double)fminf(best, kLargest), 1.0 / (double)temperature, 1.4426950408889634 / (double)temperature, (double)p.unit_bits, p.series};
   uint32_t cut = last_key, ties = kAllTies;
 
   // f(score) for all of the row's labels, and for the labels in `near`
@@ -890,6 +880,8 @@ int32_t cbd_sample_labels(cbd_sampler *s, const cbd_sample_desc *d) try {
   p.random = d->random; p.temperature = d->temperature; p.top_p = d->top_p; p.min_p = d->min_p; p.top_k = d->top_k;
   p.bits = s->bits; p.offsets = s->offsets;
   p.labels = d->labels; p.kept = d->kept; p.logprobs = d->logprobs;
+  double c = 1.0;
+  for (int k = 1; k <= 9; ++k) p.series[9 - k] = c *= 0.69314718055994531 / k;
   p.num_labels = s->N; p.num_channels = s->C; p.words = s->words; p.unit_bits = s->unit_bits;
   if (d->dtype == CBD_F32) launch_sample<float>(p, d->n, s->stream);
   else if (d->dtype == CBD_F16) launch_sample<cbd::f16>(p, d->n, s->stream);
