@@ -186,7 +186,8 @@ template <typename T, int kVec> struct Row {
 // key is left.  All sums are of integers, so their order does not matter.
 template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
   constexpr int kWaves = kBlock / 64, kVec = kHeld ? 16 / sizeof(T) : 4, kMaxCells = kHeld ? 1 : 16;
-  constexpr int kNear = !kHeld ? 8192 : kBlock == 1024 ? 512 : kList;
+  // (512 against 256 labels near the cut: 512 x 5003 in f16 with top_p 0.9 21 us against 28)
+  constexpr int kNear = !kHeld ? 8192 : 512;
   extern __shared__ float4 held[];   // kHeld: the row, by label
   __shared__ uint64_t bins[kBlock];   // of a histogram; later weights of listed labels
   // labels near the cut, or all that may be kept: key << 32 | ~label (larger: earlier in the order), in no order
@@ -728,7 +729,7 @@ struct cbd_sampler {
 namespace {
 constexpr int32_t kUpload = 1 << 15;   // entries of 8 bytes per upload slot
 
-constexpr size_t kHeldBytes = 144 * 1024;   // of LDS for a row's keys (with the kernel's own 9 KB: within 160 KB)
+constexpr size_t kHeldBytes = 144 * 1024;   // of LDS for a row's scores (with the kernel's own 13 KB: within 160 KB)
 
 template <typename T, int kBlock> size_t held_bytes(int num_labels) {   // whole turns
   const size_t turn = (size_t)kBlock * (16 / sizeof(T));
@@ -740,16 +741,25 @@ template <typename T, int kBlock, bool kHeld> void launch_rows(const cbd::Sample
   hipLaunchKernelGGL((cbd::sample_kernel<T, kBlock, kHeld>), dim3((unsigned)n), dim3(kBlock), lds, st, p);
 }
 
+// Threads per row: for few labels a step costs as much as its barriers, and two or more workgroups on a compute unit hide
+// each other's; a row alone on its compute unit with some thousand labels is faster with more threads.  With top_p 0.9,
+// fp32, threads 256 / 512 / 1024: 512 x 1500 12.1 / 13.6 / 23.9 us, 1 x 1500 9.8 / 9.5 / 11.6, 1 x 6000 16.9 / 13.6 / 14.7,
+// 256 x 6000 18.0 / 15.2 / -, 512 x 5003 in f16 28 / 28 / 31.
 template <typename T> void launch_sample(const cbd::SampleParams &p, int n, hipStream_t st) {
-  if (p.num_labels <= 8192) launch_rows<T, 256, true>(p, n, st);
+  if (p.num_labels <= 2048 || (p.num_labels <= 8192 && n > 256)) launch_rows<T, 256, true>(p, n, st);
+  else if (p.num_labels <= 8192) launch_rows<T, 512, true>(p, n, st);
   else if (held_bytes<T, 1024>(p.num_labels) <= kHeldBytes) launch_rows<T, 1024, true>(p, n, st);
   else launch_rows<T, 1024, false>(p, n, st);
 }
 
 template <typename T> hipError_t allow_held() {   // on the current device
-  const hipError_t e = hipFuncSetAttribute((const void *)cbd::sample_kernel<T, 256, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kHeldBytes);
-  if (e != hipSuccess) return e;
-  return hipFuncSetAttribute((const void *)cbd::sample_kernel<T, 1024, true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kHeldBytes);
+  const void *const kernels[] = {(const void *)cbd::sample_kernel<T, 256, true>, (const void *)cbd::sample_kernel<T, 512, true>,
+                                 (const void *)cbd::sample_kernel<T, 1024, true>};
+  for (const void *k : kernels) {
+    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)kHeldBytes);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace
