@@ -186,11 +186,19 @@ def main():
     ap.add_argument("--phases", action="store_true",
                     help="run the diagnostic build (python paper_2306_15685_amd/build.py --profile) and report the time "
                          "thread 0 of each workgroup spent in each phase of the lean frames (the stamps cost a few %%)")
+    ap.add_argument("--hidden", type=int, default=0, metavar="FEATURES",
+                    help="make every chunk's scores inside the step, by an output layer (cbd_layer_apply) over hidden vectors "
+                         "of that many features, instead of reading them from memory")
+    ap.add_argument("--draw-labels", action="store_true",
+                    help="with --hidden: also draw a label per channel and frame from the scores (cbd_sample_labels, top-p 0.95, "
+                         "the labels of the listed arcs boosted)")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--cpu-channels", type=int, default=256, help="channels of the workload the CPU checker is timed on")
     ap.add_argument("--calibrate-copy", type=int, default=0, metavar="BYTES",
                     help="only run a plain device copy of BYTES, ten times (scale for the profiler's HBM counters)")
     args = ap.parse_args()
+    if args.draw_labels and not args.hidden:
+        ap.error("--draw-labels needs --hidden")
     if args.gpus != 1:
         log("bench.py: this build decodes on one GPU only; channels are independent, so more GPUs would each "
             "hold the graph and a share of the channels (no exchange). Run with --gpus 1.")
@@ -227,7 +235,7 @@ def main():
         w = synth.scaled(w, chunk=args.chunk)
     team = args.workgroups_per_channel if args.workgroups_per_channel >= 0 else runner.default_team(w)
     t0 = time.perf_counter()
-    inp = runner.make_inputs(w)
+    inp = runner.make_inputs(w, hidden_features=args.hidden)
     torch.cuda.synchronize()
     log(f"inputs: graph {inp.g.num_states} states {inp.g.num_arcs} arcs, {w.channels} channels x "
         f"{w.segments} x {w.frames} frames x {w.num_pdfs} pdfs in {time.perf_counter() - t0:.1f} s")
@@ -236,7 +244,7 @@ def main():
                           async_partials=not args.sync_partials, workgroups_per_cu=args.workgroups_per_cu,
                           compact_records_above=args.compact_records_above, record_frames=args.record_frames,
                           tail_partials=args.tail_partials, block_threads=args.block_threads, frame_code=args.frame_code,
-                          workgroups_per_channel=team)
+                          workgroups_per_channel=team, draw=runner.Draw(top_p=0.95) if args.draw_labels else None)
     info = B.cbd_decoder_info(sess.dh)
     log(f"decoder: {info}")
 
@@ -279,7 +287,7 @@ def main():
     default_cfg = (not args.unbiased and args.context_mode == "upload" and not args.channels and not args.hash_log2
                    and not args.table_location and not args.lds_token_cap and not args.workgroups_per_cu and not args.block_threads and not args.frame_code and args.workgroups_per_channel < 0
                    and args.lookup_mode < 0 and not args.sync_partials and not args.frames and not args.chunk
-                   and not args.compact_records_above and not args.record_frames and not args.tail_partials)
+                   and not args.compact_records_above and not args.record_frames and not args.tail_partials and not args.hidden)
     traffic, traffic_at_ms = None, None
     if default_cfg and w.name in MEASURED_TRAFFIC:
         t_bytes, t_ms = MEASURED_TRAFFIC[w.name]
@@ -322,7 +330,9 @@ def main():
         out["phases"] = phase_report(B, sess, w, team)
     if inp.context_build is not None:   # Algorithm 1 on the host, outside the timed region (lists arrive rarely)
         out["context_build"] = inp.context_build
-    if not args.no_cpu_baseline:
+    if args.hidden:
+        out["config"].update(hidden_features=args.hidden, draw_labels=args.draw_labels)
+    if not args.no_cpu_baseline and not args.hidden:   # (the checker reads log-likelihoods)
         out["cpu_baseline"] = cpu_baseline(inp, min(args.cpu_channels, w.channels), w.frames)
     sess.close()
     print(json.dumps(out), flush=True)

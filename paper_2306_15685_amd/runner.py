@@ -43,18 +43,46 @@ class Inputs:
     contexts: Optional[list]  # per segment: (arc lists, offsets); None until built from `sequences`
     sequences: Optional[list] = None  # per segment: (per-channel lists of word sequences, offsets)
     context_build: Optional[Dict] = None  # host time of Algorithm 1 (filled with `contexts`)
+    # instead of log-likelihoods (`loglikes` is empty then): what the acoustic model's last layer reads, and that layer
+    hidden: Optional[list] = None   # per segment: device tensor [C, frames, features], bfloat16
+    output_layer: Optional[tuple] = None   # device tensors: weight [P, features] (bfloat16), bias [P] (fp32)
 
 
-def make_inputs(w: synth.Workload, g: Optional[synth.Graph] = None, device: str = "cuda") -> Inputs:
+@dataclass
+class Draw:
+    """Settings of a label drawn per frame from a chunk's scores (cbd_sample_labels), the same for all channels."""
+    temperature: float = 1.0
+    top_k: int = 0
+    top_p: float = 1.0
+    min_p: float = 0.0
+
+
+def make_inputs(w: synth.Workload, g: Optional[synth.Graph] = None, device: str = "cuda", hidden_features: int = 0) -> Inputs:
     """Synthetic inputs of a workload.  A workload whose graph spaces its word labels (word_period) gets its
-    biasing lists as word sequences; the arc lists are made of them by the library (contexts_from_words)."""
+    biasing lists as word sequences; the arc lists are made of them by the library (contexts_from_words).
+    hidden_features > 0: hidden vectors of that many features and an output layer instead of log-likelihoods."""
     g = g if g is not None else synth.graph_for(w)
-    L = [synth.make_loglikes(w.channels, w.frames, w.num_pdfs, w.sigma, seed_stream=(w.config_id, s), device=device)
-         for s in range(w.segments)]
+    L, hidden, output_layer = [], None, None
+    if hidden_features > 0:
+        hidden = [synth.make_hidden(w.channels, w.frames, hidden_features, seed_stream=(w.config_id, s), device=device)
+                  for s in range(w.segments)]
+        output_layer = synth.make_output_layer(hidden_features, w.num_pdfs, w.sigma, seed_stream=(w.config_id,), device=device)
+    else:
+        L = [synth.make_loglikes(w.channels, w.frames, w.num_pdfs, w.sigma, seed_stream=(w.config_id, s), device=device)
+             for s in range(w.segments)]
     if w.word_period > 0:
-        return Inputs(w, g, L, None, [synth.make_context_sequences(w, g, segment=s) for s in range(w.segments)])
+        return Inputs(w, g, L, None, [synth.make_context_sequences(w, g, segment=s) for s in range(w.segments)],
+                      hidden=hidden, output_layer=output_layer)
     ctx = [synth.make_contexts(w, g, segment=s) for s in range(w.segments)]
-    return Inputs(w, g, L, ctx)
+    return Inputs(w, g, L, ctx, hidden=hidden, output_layer=output_layer)
+
+
+def listed_labels(g: synth.Graph, contexts: tuple):
+    """The labels (pdfs) that each channel's listed arcs read, with the negated discounts (costs count down, scores up):
+    a context of the decoder as one of the sampler."""
+    lists, offs = contexts
+    read = [np.unique(g.ilabel[x]) for x in lists]
+    return [x[x > 0] - 1 for x in read], -np.asarray(offs, np.float32)
 
 
 def contexts_from_words(graph_handle, sequences: list):
@@ -79,18 +107,26 @@ class Session:
                  records_per_frame: int = 0, graph_handle=None, biased: bool = True, lds_token_cap: int = 0,
                  context_mode: str = "upload", async_partials: bool = True, workgroups_per_cu: int = 0,
                  compact_records_above: int = 0, record_frames: int = 0, tail_partials: bool = False,
-                 block_threads: int = 0, frame_code: int = 0, workgroups_per_channel: int = -1):
+                 block_threads: int = 0, frame_code: int = 0, workgroups_per_channel: int = -1,
+                 draw: Optional[Draw] = None):
         """compact_records_above / record_frames: automatic compaction of the back-pointer records, and the number
         of frames the record buffer is sized for (0: the whole utterance).  tail_partials: partial results through
         cbd_best_tails_begin / _finish (only the part of the path above what the compactions have fixed).
         context_mode: "upload" sends every segment's lists with cbd_set_contexts; "pool" loads all
-        segments' lists once with cbd_contexts_create and switches by id (Sec. 4.3)."""
+        segments' lists once with cbd_contexts_create and switches by id (Sec. 4.3).
+        Inputs with hidden vectors: the scores of each chunk are made by the output layer (cbd_layer_apply) in a buffer
+        of one chunk, in front of cbd_advance on the same stream.  draw: a label per channel and frame is drawn from
+        them as well, with the labels of the channel's listed arcs boosted; self.drawn has them (int32) and their
+        log-probabilities per segment, as device tensors [C, frames]."""
         import torch
         self.torch = torch
         self.inp = inp
         w, g = inp.w, inp.g
         self.w = w
         self.biased = biased
+        if draw is not None and inp.hidden is None:
+            raise ValueError("Session: labels are drawn from the scores of hidden vectors; these inputs have log-likelihoods")
+        self.layer = self.sampler = self.dh = None
         self.own_graph = graph_handle is None
         self.gh = graph_handle if graph_handle is not None else B.cbd_graph_load(
             g.num_states, g.num_pdfs, g.start_state, g.row_offsets, g.dst, g.ilabel, g.olabel, g.weight, g.final_cost)
@@ -124,8 +160,65 @@ class Session:
         self.time_kernels = False
         self.on_partial: Optional[Callable] = None  # called with (segment, frames_done, best_paths result)
         self.partials: list = []
+        self.draw = draw
+        self.drawn: list = []
+        if inp.hidden is not None:
+            self._make_scores(inp)
+
+    def _make_scores(self, inp: Inputs):
+        """The output layer, a chunk's scores and what drawing labels from them reads."""
+        torch, w, st = self.torch, self.w, self.stream.cuda_stream
+        weight, bias = inp.output_layer
+        self.layer = B.cbd_layer_create(weight.data_ptr(), weight.shape[1], weight.shape[0], B.DTYPES["bf16"],
+                                        weight.stride(0), bias.data_ptr(), hip_stream=st)
+        dev = weight.device
+        # a chunk of n frames is laid out [C][n][P], so that its C * n rows lie a row apart
+        self.scores = torch.empty(w.channels * min(w.chunk, w.frames) * w.num_pdfs, dtype=torch.float32, device=dev)
+        if self.draw is None:
+            return
+        self.sampler = B.cbd_sampler_create(w.channels, w.num_pdfs, hip_stream=st)
+        self.listed = [listed_labels(inp.g, c) for c in inp.contexts]
+        self.listed = [(B.pack_lists(lists), offs) for lists, offs in self.listed]
+        gen = torch.Generator(device=dev)
+        gen.manual_seed(w.config_id)
+        rows = w.channels * min(w.chunk, w.frames)
+        full = lambda v, t: torch.full((rows,), v, dtype=t, device=dev)   # noqa: E731
+        self.settings = dict(temperature=full(self.draw.temperature, torch.float32), top_k=full(self.draw.top_k, torch.int32),
+                             top_p=full(self.draw.top_p, torch.float32), min_p=full(self.draw.min_p, torch.float32))
+        lengths = {min(w.chunk, w.frames - t) for t in range(0, w.frames, w.chunk)}
+        self.row_channels = {n: torch.arange(w.channels, dtype=torch.int32, device=dev).repeat_interleave(n) for n in lengths}
+        # one number per channel and frame, in the order of the chunks' rows
+        self.random = [[torch.rand(w.channels * min(w.chunk, w.frames - t), generator=gen, device=dev)
+                        for t in range(0, w.frames, w.chunk)] for _ in range(w.segments)]
+        self.row_labels = torch.empty(rows, dtype=torch.int32, device=dev)
+        self.row_logprobs = torch.empty(rows, dtype=torch.float32, device=dev)
+        self.drawn = [(torch.empty((w.channels, w.frames), dtype=torch.int32, device=dev),
+                       torch.empty((w.channels, w.frames), dtype=torch.float32, device=dev)) for _ in range(w.segments)]
+
+    def _chunk_scores(self, s: int, t0: int, n: int):
+        """Scores of n frames of segment s, [C][n][P] in self.scores; labels drawn from them where that is asked for."""
+        w, h = self.w, self.inp.hidden[s]
+        P = w.num_pdfs
+        B.cbd_layer_apply(self.layer, w.channels, n, h[:, t0:].data_ptr(), h.stride(0), h.stride(1), self.scores.data_ptr(),
+                          n * P, P, hip_stream=self.stream.cuda_stream)
+        if self.sampler is None:
+            return
+        rows = w.channels * n
+        B.cbd_sample_labels(self.sampler, rows, self.scores.data_ptr(), P, B.DTYPES["f32"],
+                            self.random[s][t0 // w.chunk].data_ptr(), self.row_labels.data_ptr(),
+                            channels_ptr=self.row_channels[n].data_ptr(), logprobs_ptr=self.row_logprobs.data_ptr(),
+                            **{k + "_ptr": v.data_ptr() for k, v in self.settings.items()})
+        for out, of_rows in zip(self.drawn[s], (self.row_labels, self.row_logprobs)):
+            out[:, t0:t0 + n].copy_(of_rows[:rows].view(w.channels, n))
 
     def close(self):
+        if self.layer is not None:
+            self.stream.synchronize()   # (the frees want the work that uses them to have finished)
+            B.cbd_layer_free(self.layer)
+            self.layer = None
+        if self.sampler is not None:
+            B.cbd_sampler_free(self.sampler)
+            self.sampler = None
         if self.dh is not None:
             B.cbd_decoder_free(self.dh)
             self.dh = None
@@ -133,13 +226,20 @@ class Session:
             B.cbd_graph_free(self.gh)
             self.gh = None
 
-    def _advance(self, L, t0, n):
-        C, T, P = L.shape
+    def _advance(self, s, t0, n):
+        if self.layer is not None:
+            self._chunk_scores(s, t0, n)
+            P = self.w.num_pdfs
+            at, stride = self.scores.data_ptr(), n * P
+        else:
+            L = self.inp.loglikes[s]
+            C, T, P = L.shape
+            at, stride = L.data_ptr() + 4 * t0 * P, T * P
         if self.time_kernels:
             e0 = self.torch.cuda.Event(enable_timing=True)
             e1 = self.torch.cuda.Event(enable_timing=True)
             e0.record(self.stream)
-        B.cbd_advance(self.dh, self.all, L.data_ptr() + 4 * t0 * P, T * P, n)
+        B.cbd_advance(self.dh, self.all, at, stride, n)
         if self.time_kernels:
             e1.record(self.stream)
             self.advance_events.append((e0, e1))
@@ -162,13 +262,15 @@ class Session:
             elif s == 0:
                 B.cbd_set_contexts(self.dh, self.all, [np.zeros(0, np.int32)] * w.channels,
                                    np.zeros(w.channels, np.float32))
+            if self.sampler is not None:
+                packed, boost = self.listed[s]
+                B.cbd_sampler_set_contexts(self.sampler, self.all, None, boost if self.biased else 0 * boost, packed=packed)
             B.cbd_reset_channels(self.dh, self.all)
-            L = self.inp.loglikes[s]
             t = 0
             pending = None   # (ticket, frames done) of the partial request still in flight
             while t < w.frames:
                 n = min(w.chunk, w.frames - t)
-                self._advance(L, t, n)
+                self._advance(s, t, n)
                 t += n
                 if pending_final is not None:
                     # the previous utterance's final result: collected now that this utterance's first chunk is

@@ -242,6 +242,30 @@ def make_loglikes(channels: int, frames: int, num_pdfs: int, sigma: float,
     return torch.log_softmax(x, dim=-1)
 
 
+def make_hidden(channels: int, frames: int, features: int, seed_stream: Tuple[int, ...] = (0,), device: str = "cpu"):
+    """bfloat16 tensor [channels, frames, features] of N(0, 1): what an acoustic model's last layer reads."""
+    import torch
+
+    g = torch.Generator(device=device)
+    g.manual_seed(int(np.random.SeedSequence([BASE_SEED, 8, *seed_stream]).generate_state(1, np.uint64)[0] >> 1))
+    out = torch.empty((channels, frames, features), device=device, dtype=torch.bfloat16)
+    for c in range(channels):   # (a channel at a time: the fp32 numbers are twice as large)
+        out[c] = torch.randn((frames, features), generator=g, device=device, dtype=torch.float32)
+    return out
+
+
+def make_output_layer(features: int, num_pdfs: int, sigma: float, seed_stream: Tuple[int, ...] = (0,), device: str = "cpu"):
+    """Weights [num_pdfs, features] (bfloat16) and bias [num_pdfs] (fp32) that make scores of N(0, sigma^2) out of
+    make_hidden's vectors, less the logarithm of their mean mass: log-likelihoods but for a small constant per frame."""
+    import torch
+
+    g = torch.Generator(device=device)
+    g.manual_seed(int(np.random.SeedSequence([BASE_SEED, 9, *seed_stream]).generate_state(1, np.uint64)[0] >> 1))
+    weight = torch.randn((num_pdfs, features), generator=g, device=device, dtype=torch.float32) * (sigma / features ** 0.5)
+    bias = torch.full((num_pdfs,), -(float(np.log(num_pdfs)) + 0.5 * sigma * sigma), device=device)
+    return weight.to(torch.bfloat16), bias
+
+
 def word_arcs(g: Graph) -> np.ndarray:
     return np.nonzero(g.olabel != 0)[0].astype(np.int32)
 
