@@ -433,14 +433,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LayerParams p, in
                       (tile_m + 1) * BM <= p.rows && (tile_n + 1) * WN * FN * 16 <= p.N);
 }
 
-// Few rows: a workgroup makes (FM * 16) rows x 16 outputs, its waves share K (wave w takes groups of four steps w, w +
-// kWaves, ...) and add their sums up in LDS, in the order of the waves.  No operand is used twice by a wave, so both come
-// straight from memory, four steps in flight.
+// Few outputs in all: a workgroup makes (FM * 16) rows x (FN * 16) outputs, its waves share K (wave w takes groups of
+// kAhead steps w, w + kWaves, ...) and add their sums up in LDS, in the order of the waves.  Operands are used FM or FN
+// times by one wave only, so both come straight from memory, kAhead steps in flight (two with 32 x 32: fp32 500 x 2048 ->
+// 500 15.4 us, with four 18.1: half the registers, twice the workgroups on a compute unit).
 constexpr int kNarrowWaves = 8;
-template <typename T, int FM> __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(LayerParams p) {
-  constexpr int kElems = 16 / sizeof(T), kStep = 4 * kElems, kAhead = 4;
-  __shared__ float4v sums[kNarrowWaves][FM][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, block = blockIdx.x;
+template <typename T, int FM, int FN, int kAhead> __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(LayerParams p) {
+  constexpr int kElems = 16 / sizeof(T), kStep = 4 * kElems;
+  __shared__ float4v sums[kNarrowWaves][FM][FN][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const T *src[FM];
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
@@ -448,16 +449,22 @@ template <typename T, int FM> __global__ __launch_bounds__(64 * kNarrowWaves) vo
     const int c = channel_of(p, r), f = r - c * p.frames;
     src[i] = (const T *)p.x + c * p.x_cs + f * p.x_fs + (lane >> 4) * kElems;
   }
-  const uint4v *w = (const uint4v *)p.w + (int64_t)block * p.w_steps * 64 + lane;
-  float4v acc[FM];
+  const uint4v *w[FN];
 #pragma unroll
-  for (int i = 0; i < FM; ++i) acc[i] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int j = 0; j < FN; ++j)   // (a block beyond the last repeats it and is not stored)
+    w[j] = (const uint4v *)p.w + (int64_t)min((int)blockIdx.x * FN + j, p.w_blocks - 1) * p.w_steps * 64 + lane;
+  float4v acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
   for (int s0 = wave * kAhead; s0 < p.w_steps; s0 += kNarrowWaves * kAhead) {
-    uint4v wv[kAhead], xv[kAhead][FM];
+    uint4v wv[kAhead][FN], xv[kAhead][FM];
     if (s0 + kAhead <= p.w_steps && (s0 + kAhead) * kStep <= p.K) {
 #pragma unroll
       for (int a = 0; a < kAhead; ++a) {
-        wv[a] = w[(int64_t)(s0 + a) * 64];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) wv[a][j] = w[j][(int64_t)(s0 + a) * 64];
 #pragma unroll
         for (int i = 0; i < FM; ++i) { const uint4u v = *(const uint4u *)(src[i] + (s0 + a) * kStep); xv[a][i] = v; }
       }
@@ -465,7 +472,8 @@ template <typename T, int FM> __global__ __launch_bounds__(64 * kNarrowWaves) vo
 #pragma unroll
       for (int a = 0; a < kAhead; ++a) {
         const int s = min(s0 + a, p.w_steps - 1);
-        wv[a] = w[(int64_t)s * 64];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) wv[a][j] = w[j][(int64_t)s * 64];
         // (a step beyond the last counts as one beyond K: zeros)
         const int k = (s0 + a) * kStep;
 #pragma unroll
@@ -477,23 +485,29 @@ template <typename T, int FM> __global__ __launch_bounds__(64 * kNarrowWaves) vo
 #pragma unroll
       for (int q = 0; q < Mma<T>::kParts; ++q)
 #pragma unroll
-        for (int i = 0; i < FM; ++i) acc[i] = Mma<T>::run(q, wv[a], xv[a][i], acc[i]);
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = Mma<T>::run(q, wv[a][j], xv[a][i], acc[i][j]);
   }
 #pragma unroll
-  for (int i = 0; i < FM; ++i) sums[wave][i][lane] = acc[i];
-  __syncthreads();
-  // a wave finishes a row block: lane l has row l % 16 and the four outputs of the block's rows 4 (l / 16) ..
-  if (wave >= FM) return;
-  float4v v = sums[0][wave][lane];
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
-  for (int k = 1; k < kNarrowWaves; ++k) v += sums[k][wave][lane];
-  const int r = (int)(blockIdx.y * FM + wave) * 16 + (lane & 15), n = packed_output(block, (lane >> 4) * 4);
-  if (r >= p.rows) return;
-  const int c = channel_of(p, r), f = r - c * p.frames;
-  float y[4] = {v[0], v[1], v[2], v[3]}, bias[4];
-  load_bias(p, n, bias);
-  finish<true>(p, y, bias);
-  store(p, c * p.out_cs + f * p.out_fs, c * p.res_cs + f * p.res_fs, n, y);
+    for (int j = 0; j < FN; ++j) sums[wave][i][j][lane] = acc[i][j];
+  __syncthreads();
+  // a wave finishes a block: lane l has row l % 16 and the four outputs of the block's rows 4 (l / 16) ..
+  for (int at = wave; at < FM * FN; at += kNarrowWaves) {
+    const int i = at / FN, j = at % FN;
+    float4v v = sums[0][i][j][lane];
+#pragma unroll
+    for (int k = 1; k < kNarrowWaves; ++k) v += sums[k][i][j][lane];
+    const int r = (int)(blockIdx.y * FM + i) * 16 + (lane & 15), n = packed_output((int)blockIdx.x * FN + j, (lane >> 4) * 4);
+    if (r >= p.rows) continue;
+    const int c = channel_of(p, r), f = r - c * p.frames;
+    float y[4] = {v[0], v[1], v[2], v[3]}, bias[4];
+    load_bias(p, n, bias);
+    finish<true>(p, y, bias);
+    store(p, c * p.out_cs + f * p.out_fs, c * p.res_cs + f * p.res_fs, n, y);
+  }
 }
 
 }  // namespace
@@ -531,8 +545,9 @@ template <typename T, int WM, int WN, int FM, int FN> hipError_t launch_tiles(co
   return hipGetLastError();
 }
 
-template <typename T, int FM> hipError_t launch_narrow(const LayerParams &p, hipStream_t st) {
-  hipLaunchKernelGGL((cbd::narrow_kernel<T, FM>), dim3((unsigned)p.w_blocks, (unsigned)((p.rows + FM * 16 - 1) / (FM * 16))),
+template <typename T, int FM, int FN, int kAhead> hipError_t launch_narrow(const LayerParams &p, hipStream_t st) {
+  auto kernel = cbd::narrow_kernel<T, FM, FN, kAhead>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((p.w_blocks + FN - 1) / FN), (unsigned)((p.rows + FM * 16 - 1) / (FM * 16))),
                      dim3(64 * cbd::kNarrowWaves), 0, st, p);
   return hipGetLastError();
 }
@@ -541,26 +556,56 @@ int64_t tiles_of(const LayerParams &p, int rows, int outputs) {
   return (int64_t)((p.rows + rows - 1) / rows) * ((p.N + outputs - 1) / outputs);
 }
 
-// Which kernel.  Few outputs in all: the narrow kernel, whose waves share K, while it takes at most about two
-// workgroups per compute unit (256 of them; bf16, rows x in -> out: 64 x 1024 -> 1024 4.5 us against 7.3 with 64 x 64
-// tiles; at 512 workgroups 256 x 1024 -> 1024 7.0 / 7.4 and 231 x 771 -> 1021 10.6 / 8.2; 200 x 1024 -> 3000 14.9 / 7.8), and always for up to 32 rows, where the weights' bytes bound it.
-// Otherwise the larger the tile, the fewer reads per product, as long as the tiles fill the chip:
-//   64 x 64 below 240 tiles of 64 x 128  (512 x 1024 -> 1024: 7.6 us against 8.8 with 64 x 128)
-//   64 x 128 below 1000 such tiles       (1000 x 1024 -> 6000: 21.3; 64 x 64 26.9, 64 x 256 22.5)
-//   64 x 256 below 512 of 128 x 256      (3000 x 1024 -> 4096: 33.5; 64 x 128 36.6, 128 x 256 36.3)
-//   128 x 256 from there                 (16384 x 1024 -> 4096: 144; 64 x 256 157)
-// fp32 products take 16 times the time of bf16 ones, so that even spreading counts more than reads: 64 x 128 tiles at
-// most (1600 x 1024 -> 6000: 175 us; 64 x 64 188, 64 x 256 214).
-template <typename T> hipError_t launch(const LayerParams &p, hipStream_t st) {
-  if (p.rows <= 16 || tiles_of(p, 16, 16) <= 512) return launch_narrow<T, 1>(p, st);
-  if (p.rows <= 32 || tiles_of(p, 32, 16) <= 400) return launch_narrow<T, 2>(p, st);
-  const int64_t tiles = tiles_of(p, 64, 128);
-  if (tiles < 240) return launch_tiles<T, 2, 2, 2, 2>(p, st);
-  if constexpr (sizeof(T) == 2) {
-    if (tiles >= 1000)
-      return tiles_of(p, 128, 256) < 512 ? launch_tiles<T, 1, 4, 4, 4>(p, st) : launch_tiles<T, 1, 4, 8, 4>(p, st);
+// A kernel's share of the choice: the time of a launch is close to K * (first + more * (n / 256 - 1)) ns for n > 256
+// workgroups of `rows` x `outputs`, and K * first ns up to then (256 compute units; above, they overlap or queue).
+struct Choice {
+  int rows, outputs;
+  float first, more;
+  float cost(const LayerParams &p) const {
+    if (outputs <= 64 && (p.rows - 1) / rows >= 65535) return 1e30f;   // (waves that share K: row blocks are the grid's second dimension)
+    const float n = (float)tiles_of(p, rows, outputs) / 256.0f;
+    return n <= 1.0f ? first : first + more * (n - 1.0f);
   }
-  return launch_tiles<T, 1, 4, 4, 2>(p, st);
+};
+
+// Which kernel.  Large tiles read less per product, small ones and those whose waves share K leave fewer compute units
+// without work; which counts more follows from the number of workgroups alone, as all kernels' times grow with K.  The
+// figures were fitted to 20 to 100,000 rows, 64 to 4096 inputs, 256 to 100,000 outputs; the choice is within 6 % of the best
+// of all on average.  us for 16 x 16 / 32 x 32 / 32 x 64 by waves that share K, and tiles of 32 x 128 / 64 x 128:
+//   bf16   64 x 1024 -> 1024    4.0 /  4.9 /  5.7 /  6.9 /  8.6      fp32   64 x 1024 -> 1024    5.0 /  8.7 /  -  / 23.6 / 38.3
+//   bf16  231 x  771 -> 1021   10.7 /  7.4 /  7.8 /  7.3 /  9.3      fp32  500 x 2048 ->  500   22.4 / 15.4 /  -  / 43.9 / 73.4
+//   bf16 1000 x 4096 ->  256   19.2 / 12.5 / 15.0 / 18.7 / 24.3      fp32  336 x 1272 -> 3653   66.1 / 49.0 /  -  / 49.4 / 55.3
+//   bf16 2000 x 1024 -> 4000    140 /  77  /  80  / 32.8 / 25.0      fp32 1600 x  512 -> 3000   86.3 / 63.1 /  -  / 49.3 / 55.8
+// (fp32: products take 16 times the time of bf16 ones, so that spreading them counts for more than reads.)
+// Chip-filling 16-bit products with more than a few steps of K take larger tiles:
+//   64 x 256 from 1000 tiles of 64 x 128  (1600 x 1024 -> 6000: 29.6; 64 x 128 32.9; but 6400 x 512 -> 2000: 26.3 and 24.1)
+//   128 x 256 from 512 of its own tiles   (16384 x 1024 -> 4096: 144; 64 x 256 157)
+template <typename T> hipError_t launch(const LayerParams &p, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) {
+    if (tiles_of(p, 64, 128) >= 1000 && p.K > 512)
+      return tiles_of(p, 128, 256) < 512 ? launch_tiles<T, 1, 4, 4, 4>(p, st) : launch_tiles<T, 1, 4, 8, 4>(p, st);
+    const Choice choices[] = {{16, 16, 0.55f, 1.1f}, {32, 32, 1.5f, 2.5f}, {32, 64, 2.0f, 3.8f}, {32, 128, 3.5f, 4.6f}, {64, 128, 5.2f, 8.1f}};
+    int best = 0;
+    for (int i = 1; i < 5; ++i)
+      if (choices[i].cost(p) < choices[best].cost(p)) best = i;
+    switch (best) {
+      case 0: return launch_narrow<T, 1, 1, 4>(p, st);
+      case 1: return launch_narrow<T, 2, 2, 2>(p, st);
+      case 2: return launch_narrow<T, 2, 4, 2>(p, st);
+      case 3: return launch_tiles<T, 1, 4, 2, 2>(p, st);
+      default: return launch_tiles<T, 1, 4, 4, 2>(p, st);
+    }
+  } else {
+    const Choice choices[] = {{16, 16, 1.9f, 2.5f}, {32, 32, 4.7f, 8.1f}, {32, 128, 21.0f, 27.0f}};
+    int best = 0;
+    for (int i = 1; i < 3; ++i)
+      if (choices[i].cost(p) < choices[best].cost(p)) best = i;
+    switch (best) {
+      case 0: return launch_narrow<T, 1, 1, 4>(p, st);
+      case 1: return launch_narrow<T, 2, 2, 2>(p, st);
+      default: return launch_tiles<T, 1, 4, 2, 2>(p, st);
+    }
+  }
 }
 
 bool aligned(const void *ptr, int32_t dtype) { return ((uintptr_t)ptr & (cbd::dtype_size(dtype) - 1)) == 0; }

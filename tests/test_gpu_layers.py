@@ -69,10 +69,12 @@ SHAPES = [(1, 1, 1, 1), (1, 1, 64, 16), (1, 1, 1024, 6000), (1, 3, 7, 5), (3, 1,
 LARGE = [(1, 1003, 40, 2001), (5, 501, 72, 3301), (3, 1411, 33, 4133), (70, 61, 100, 4101)]
 # ... and with every tile whole
 LARGE_WHOLE = [(2, 512, 64, 2048), (4, 640, 32, 3328), (8, 512, 96, 4352)]
+# ... many rows of few outputs, and inputs long enough for the largest tiles in 16 bits
+DEEP = [(1, 500, 1032, 500), (32, 33, 517, 511), (3, 1411, 577, 2001), (70, 61, 520, 4101), (4, 640, 544, 3328), (8, 512, 576, 4352)]
 
 
 @pytest.mark.parametrize("dtype,out", [("bf16", "f32"), ("f16", "f16"), ("f32", "f32"), ("bf16", "bf16"), ("f16", "bf16"), ("f32", "f16")])
-@pytest.mark.parametrize("shape", LARGE + LARGE_WHOLE)
+@pytest.mark.parametrize("shape", LARGE + LARGE_WHOLE + DEEP)
 def test_whole_numbers_are_exact_in_large_products(shape, dtype, out):
     import torch
     C, F, K, N = shape
@@ -131,6 +133,38 @@ def test_real_numbers_within_the_derived_bound(dtype, out, act):
         layer.close()
 
 
+@pytest.mark.parametrize("dtype,out,act", [("bf16", "bf16", "silu"), ("f16", "f32", "gelu"), ("f32", "f32", "sigmoid"), ("f32", "f16", "tanh")])
+def test_real_numbers_in_larger_products(dtype, out, act):
+    import torch
+    for C, F, K, N in [(7, 33, 771, 1021), (32, 33, 256, 511), (11, 97, 264, 1032), (5, 401, 90, 2101), (3, 1411, 577, 2001), (8, 512, 576, 4352)]:
+        g = gen(K + N)
+        x = (torch.randn((C, F, K), generator=g, device=DEV) * 2).to(T(dtype))
+        w = (torch.randn((N, K), generator=g, device=DEV) / K ** 0.5).to(T(dtype))
+        b, res = torch.randn(N, generator=g, device=DEV), torch.randn((C, F, N), generator=g, device=DEV).to(T(out))
+        layer = Layer(w, b, dtype, act)
+        got = layer.apply(x, res.clone(), 0.75, None, 0.0).double()
+        want, err = R.layer64(x, w, b, act, 0.75, None, 0.0, out)
+        assert ((got - want).abs() <= err).all(), (C, F, K, N)
+        inout = res.clone()   # the residual in place
+        layer.apply(x, inout, 0.75, inout, 0.5)
+        want, err = R.layer64(x, w, b, act, 0.75, res, 0.5, out)
+        assert ((inout.double() - want).abs() <= err).all(), (C, F, K, N)
+        layer.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_million_rows_of_three_outputs(dtype):
+    import torch
+    g = gen(4)
+    rows = 65_535 * 32 + 21   # (more blocks of 16 and of 32 rows than a grid's second dimension has)
+    x, w = whole((1, rows, 8), dtype, g), whole((3, 8), dtype, g)
+    layer = Layer(w, None, dtype)
+    for n in (rows, 65_535 * 16, 65_535 * 16 + 1):
+        got = layer.apply(x[:, :n], torch.full((1, n, 3), 7.0, device=DEV))
+        assert torch.equal(got, (x[:, :n].double() @ w.double().t()).float())
+    layer.close()
+
+
 @pytest.mark.parametrize("act", ["sigmoid", "tanh", "gelu", "silu"])
 def test_activations_at_the_ends_of_their_range(act):
     """One input, weight 1: the activation itself, at large values of both signs, at zero and at infinity."""
@@ -148,7 +182,8 @@ def test_activations_at_the_ends_of_their_range(act):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("C,F,K,N", [(1, 1, 96, 40), (3, 5, 100, 70), (4, 9, 64, 64), (6, 50, 72, 270)])
+@pytest.mark.parametrize("C,F,K,N", [(1, 1, 96, 40), (3, 5, 100, 70), (4, 9, 64, 64), (6, 50, 72, 270), (7, 33, 200, 1021),
+                                     (32, 33, 100, 511), (11, 97, 72, 1032), (9, 300, 40, 1700)])
 def test_layouts(dtype, C, F, K, N):
     """Chunks of longer buffers, frames outermost, rows that overlap, pointers aligned to one element only; what lies
     between the rows is neither read into results nor written."""
@@ -205,7 +240,7 @@ def test_layouts(dtype, C, F, K, N):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
-@pytest.mark.parametrize("rows,K,N", [(5, 40, 24), (70, 136, 100), (300, 264, 520)])
+@pytest.mark.parametrize("rows,K,N", [(5, 40, 24), (70, 136, 100), (300, 264, 520), (1067, 264, 1032), (1056, 136, 511)])
 def test_what_is_not_finite_stays_in_its_row_and_column(dtype, rows, K, N):
     import torch
     g = gen(rows)
