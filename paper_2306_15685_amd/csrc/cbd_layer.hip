@@ -326,7 +326,10 @@ template <typename T> __global__ __launch_bounds__(256) void pack_weight_kernel(
 
 // Tiles.  A workgroup of WM x WN waves makes (WM * FM * 16) rows x (WN * FN * 16) outputs; a wave FM x FN blocks of 16 x
 // 16.  Input rows go through LDS, 128 bytes of K at a time, two buffers; weights come straight from the packed layout
-// into registers, one such step ahead.
+// into registers, one such step ahead: no two waves of a workgroup read the same weights, so LDS would only delay them,
+// and its bandwidth is left to the rows.  Measured (12800 rows): 1024 -> 6000 in bf16 to fp32 179 us, 1024 -> 4096 with
+// silu 113 us (880 and 950 TFLOP/s; the matrix units are busy half of the cycles: the stores of a tile's results and its
+// first loads are not covered by products), fp32 1600 x 512 -> 3000 49.5 us (99 TFLOP/s, busy 73 %: the last of 1200 tiles).
 template <typename T, typename O, bool kActivation, int WM, int WN, int FM, int FN>
 __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LayerParams p, int tiles_m, int tiles_n) {
   constexpr int kThreads = 64 * WM * WN, BM = WM * FM * 16, kElems = 16 / sizeof(T), kTileK = 8 * kElems;
@@ -436,7 +439,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LayerParams p, in
 // Few outputs in all: a workgroup makes (FM * 16) rows x (FN * 16) outputs, its waves share K (wave w takes groups of
 // kAhead steps w, w + kWaves, ...) and add their sums up in LDS, in the order of the waves.  Operands are used FM or FN
 // times by one wave only, so both come straight from memory, kAhead steps in flight (two with 32 x 32: fp32 500 x 2048 ->
-// 500 15.4 us, with four 18.1: half the registers, twice the workgroups on a compute unit).
+// 500 15.4 us, with four 18.1: half the registers, twice the workgroups on a compute unit).  Bound by the latency of its
+// few loads: 1 x 1024 -> 6000 in bf16 5.1 us (12.3 MB, 2.4 TB/s), 32 x 2048 -> 512 5.5 us, a fill of one number 3.4.
 constexpr int kNarrowWaves = 8;
 template <typename T, int FM, int FN, int kAhead> __global__ __launch_bounds__(64 * kNarrowWaves) void narrow_kernel(LayerParams p) {
   constexpr int kElems = 16 / sizeof(T), kStep = 4 * kElems;

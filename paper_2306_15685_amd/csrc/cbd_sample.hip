@@ -184,6 +184,12 @@ template <typename T, int kVec> struct Row {
 // the interval of keys in question, one bin a thread: counts or masses per bin, their running sum from the best key
 // down, and the bin where it passes the border is the next interval, narrowed to the keys that occur in it, until one
 // key is left.  All sums are of integers, so their order does not matter.
+//
+// Measured: 2048 x 6000 fp32 with min_p 28 us (the copy of its 49 MB takes 10), 64 x 20000 bf16 with top_k 50 and top_p 19,
+// 512 x 5003 fp16 with top_p 21, 256 x 200,000 fp32 with top_p 228 (copy 42): there the row is read three times (largest
+// score; masses of the bins; sums of what is kept and the labels near the cut), and the last two take some 26 vector
+// instructions of four cycles per label for its weight, 81 million in all: 132 us of issue.  Rows in LDS are bound by the
+// same instructions and by the barriers between steps.
 template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
   constexpr int kWaves = kBlock / 64, kVec = kHeld ? 16 / sizeof(T) : 4, kMaxCells = kHeld ? 1 : 16;
   // (512 against 256 labels near the cut: 512 x 5003 in f16 with top_p 0.9 21 us against 28)
