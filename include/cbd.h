@@ -424,7 +424,8 @@ typedef struct cbd_layer_desc {
 
 /*
  * Lays the weights out on the current HIP device, on `hip_stream` (a hipStream_t of that device, NULL = the null stream),
- * and waits for it: the caller's arrays are free again when the call returns.  Not while the stream is being captured.
+ * and waits for it: the caller's arrays are free again when the call returns.  Not while the stream is being captured.  At
+ * most 64 GB of weights.
  */
 int32_t cbd_layer_create(const cbd_layer_desc *desc, void *hip_stream, cbd_layer **out);
 /* Frees the layer; work that still uses it must have finished. */
@@ -432,7 +433,7 @@ int32_t cbd_layer_free(cbd_layer *l);
 
 typedef struct cbd_layer_io {
   int32_t n_channels;           /* row (channel i, frame f) of an array X is at X + i*channel_stride + f*frame_stride */
-  int32_t n_frames;             /* (elements); n_channels or n_frames = 0: nothing to do */
+  int32_t n_frames;             /* (elements); n_channels or n_frames = 0: nothing to do; n_channels * n_frames <= 2^29 - 256 */
   const void *input;            /* DEVICE, elements of the layer's dtype */
   int64_t input_channel_stride; /* >= 0; rows may overlap (a context of frames spliced into one row) */
   int64_t input_frame_stride;
@@ -477,7 +478,7 @@ typedef struct cbd_sampler cbd_sampler; /* opaque; owns the channels' lists */
 /* For up to num_channels lists (>= 1) over rows of num_labels scores (1 .. 1048576), on the current HIP device; all work
  * is enqueued on `hip_stream` (a hipStream_t of that device, NULL = the null stream). */
 int32_t cbd_sampler_create(int32_t num_channels, int32_t num_labels, void *hip_stream, cbd_sampler **out);
-/* Waits for the stream, then frees. */
+/* Waits for the stream, then frees.  Not while the stream is being captured. */
 int32_t cbd_sampler_free(cbd_sampler *s);
 
 /*

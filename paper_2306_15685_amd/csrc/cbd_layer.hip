@@ -542,6 +542,7 @@ template <typename F> void with_output(const LayerParams &p, F f) {
 
 template <typename T, int WM, int WN, int FM, int FN> hipError_t launch_tiles(const LayerParams &p, hipStream_t st) {
   const int tiles_m = (p.rows + WM * FM * 16 - 1) / (WM * FM * 16), tiles_n = (p.N + WN * FN * 16 - 1) / (WN * FN * 16);
+  if ((int64_t)tiles_m * tiles_n * (64 * WM * WN) > 0xFFFFFFFFll) return hipErrorInvalidConfiguration;   // (threads of a launch; up to 128 outputs never)
   with_output(p, [&](auto o, auto act) {
     hipLaunchKernelGGL((cbd::tile_kernel<T, decltype(o), decltype(act)::value, WM, WN, FM, FN>), dim3((unsigned)tiles_m * (unsigned)tiles_n),
                        dim3(64 * WM * WN), 0, st, p, tiles_m, tiles_n);
@@ -646,6 +647,11 @@ int32_t cbd_layer_create(const cbd_layer_desc *desc, void *hip_stream, cbd_layer
   if (stride < desc->in_features || stride > (int64_t)1 << 40) return fail(CBD_E_INVALID, "layer: weight_stride");
   if (!aligned(desc->weight, desc->dtype) || !aligned(desc->bias, CBD_F32))
     return fail(CBD_E_INVALID, "layer: weight or bias not aligned to its elements");
+  const int32_t step = 64 / (int32_t)cbd::dtype_size(desc->dtype);
+  const int32_t blocks = (desc->out_features + 31) / 32 * 2;
+  const int32_t steps = (desc->in_features + 2 * step - 1) / (2 * step) * 2;   // (tiles take two steps at a time)
+  const int64_t total = (int64_t)blocks * steps * 64;   // 16-byte pieces, one per thread of a launch
+  if (total > 0xFFFFFF00ll) return fail(CBD_E_INVALID, "layer: more than 64 GB of weights");
   hipStream_t st = (hipStream_t)hip_stream;
   int device = 0;
   HIPCHK(hipGetDevice(&device));
@@ -659,10 +665,7 @@ int32_t cbd_layer_create(const cbd_layer_desc *desc, void *hip_stream, cbd_layer
   } guard{l};
   l->device = device;
   l->K = desc->in_features; l->N = desc->out_features; l->dtype = desc->dtype; l->act = desc->activation;
-  const int32_t step = 64 / (int32_t)cbd::dtype_size(l->dtype);
-  l->blocks = (l->N + 31) / 32 * 2;
-  l->steps = (l->K + 2 * step - 1) / (2 * step) * 2;   // (tiles take two steps at a time)
-  const int64_t total = (int64_t)l->blocks * l->steps * 64;   // 16-byte pieces
+  l->blocks = blocks; l->steps = steps;
   HIPCHK(dmalloc((char **)&l->w, (size_t)total * 16, nullptr));
   const dim3 grid((unsigned)((total + 255) / 256));
   cbd::uint4v *w = (cbd::uint4v *)l->w;
@@ -701,7 +704,7 @@ int32_t cbd_layer_apply(const cbd_layer *l, const cbd_layer_io *io, void *hip_st
     return fail(CBD_E_INVALID, "layer_apply: scales must be finite");
   const int64_t n = io->n_channels, m = io->n_frames, rows = n * m;
   if (rows == 0) return CBD_OK;
-  if (rows > 0x7FFFFF00) return fail(CBD_E_INVALID, "layer_apply: too many rows");
+  if (rows > (1 << 29) - 256) return fail(CBD_E_INVALID, "layer_apply: too many rows");
   if (!io->input || !io->output) return fail(CBD_E_INVALID, "layer_apply: null input or output");
   if (!aligned(io->input, l->dtype) || !aligned(io->output, io->output_dtype) || !aligned(io->residual, io->output_dtype))
     return fail(CBD_E_INVALID, "layer_apply: a pointer is not aligned to its elements");

@@ -25,6 +25,7 @@ struct SampleParams {
   const float *offsets;      // per channel
   int32_t *labels, *kept;
   float *logprobs;
+  int32_t first_row;         // of this launch
   int32_t num_labels, num_channels, words;   // words: 32-bit words of a channel's bits
   int32_t unit_bits;         // weights are summed in units of 2^-unit_bits
   double series[9];          // ln(2)^k / k!, k = 9 .. 1 (arguments: they stay in scalar registers)
@@ -202,7 +203,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   __shared__ uint32_t cell_ties[kWaves * kMaxCells], wave_a[kWaves], wave_b[kWaves], wave_c[kWaves];
   __shared__ uint64_t pick_before;
   __shared__ uint32_t pick_bin, pick_count, n_near;
-  const int r = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = p.num_labels;
+  const int r = p.first_row + (int)blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = p.num_labels;
   const int ch = p.channels ? p.channels[r] : r;
   auto write = [&](int label, float lp, int kept) {   // (by one thread)
     p.labels[r] = label;
@@ -813,6 +814,7 @@ int32_t cbd_sampler_create(int32_t num_channels, int32_t num_labels, void *hip_s
 
 int32_t cbd_sampler_free(cbd_sampler *s) {
   if (!s) return CBD_OK;
+  if (cbd::is_capturing(s->stream)) return fail(CBD_E_INVALID, "sampler_free: the stream is being captured");
   (void)hipStreamSynchronize(s->stream);
   if (s->bits) (void)hipFree(s->bits);
   if (s->offsets) (void)hipFree(s->offsets);
@@ -899,10 +901,16 @@ int32_t cbd_sample_labels(cbd_sampler *s, const cbd_sample_desc *d) try {
   double c = 1.0;
   for (int k = 1; k <= 9; ++k) p.series[9 - k] = c *= 0.69314718055994531 / k;
   p.num_labels = s->N; p.num_channels = s->C; p.words = s->words; p.unit_bits = s->unit_bits;
-  if (d->dtype == CBD_F32) launch_sample<float>(p, d->n, s->stream);
-  else if (d->dtype == CBD_F16) launch_sample<cbd::f16>(p, d->n, s->stream);
-  else launch_sample<cbd::bf16>(p, d->n, s->stream);
-  HIPCHK(hipGetLastError());
+  constexpr int32_t kRows = 1 << 21;   // (a launch has fewer than 2^32 threads)
+  for (int32_t done = 0; done < d->n;) {
+    const int32_t m = std::min(kRows, d->n - done);
+    p.first_row = done;
+    if (d->dtype == CBD_F32) launch_sample<float>(p, m, s->stream);
+    else if (d->dtype == CBD_F16) launch_sample<cbd::f16>(p, m, s->stream);
+    else launch_sample<cbd::bf16>(p, m, s->stream);
+    HIPCHK(hipGetLastError());
+    done += m;
+  }
   return CBD_OK;
 } catch (const std::exception &e) {
   return fail(CBD_E_HIP, std::string("sample_labels: ") + e.what());

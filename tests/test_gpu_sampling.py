@@ -282,6 +282,8 @@ def test_captured_call_replays_with_new_values():
             s.lists([0], [[1]], [1.0])
         with pytest.raises(B.CbdError):
             B.cbd_sampler_create(C, N, hip_stream=stream.cuda_stream)
+        with pytest.raises(B.CbdError):
+            B.cbd_sampler_free(s.h)
     for k in range(4):
         rows, uu, pp = rng.normal(0, 2, (C, N)).astype(np.float32), rng.random(C).astype(np.float32), rng.uniform(0.3, 0.95, C).astype(np.float32)
         x.copy_(torch.from_numpy(rows)); u.copy_(torch.from_numpy(uu)); p.copy_(torch.from_numpy(pp))  # noqa: E702
@@ -295,6 +297,64 @@ def test_captured_call_replays_with_new_values():
         for r in range(C):
             check([v[r] for v in got], R.sample_row(rows[r], float(uu[r]), top_p=float(pp[r]), listed=lists[r], offset=2.0), N, (k, r))
     s.close()
+
+
+@pytest.mark.parametrize("with_channels", [True, False])
+def test_more_rows_than_one_launch_takes(with_channels):
+    """2^21 + 70 rows of five scores; row i's best label is i mod 5."""
+    import torch
+    n, N = 2 ** 21 + 70, 5
+    s = Sampler(n if not with_channels else 3, N)
+    at = torch.arange(n, device=DEV, dtype=torch.int32)
+    x = torch.full((n, N), -100.0, device=DEV, dtype=torch.float16)
+    x.scatter_(1, (at % N).long()[:, None], 100.0)
+    u, labels, kept = torch.rand(n, device=DEV), torch.full((n + 1,), 77, device=DEV, dtype=torch.int32), torch.zeros(n, device=DEV, dtype=torch.int32)
+    top_p = torch.full((n,), 0.5, device=DEV)
+    which = 2 * (at >= 2 ** 21).int()
+    # raised by 300: of channel 2 (the rows behind the first 2^21), or of one row there and one before it
+    s.lists([2], [[3]], [300.0]) if with_channels else s.lists([2 ** 21 - 1, 2 ** 21 + 66], [[3], [4]], [300.0, 300.0])
+    B.cbd_sample_labels(s.h, n, x.data_ptr(), N, B.DTYPES["f16"], u.data_ptr(), labels.data_ptr(), top_p_ptr=top_p.data_ptr(),
+                        channels_ptr=which.data_ptr() if with_channels else 0, kept_ptr=kept.data_ptr())
+    torch.cuda.synchronize()
+    want = at % N
+    if with_channels:
+        want[2 ** 21:] = 3
+    else:
+        want[2 ** 21 - 1], want[2 ** 21 + 66] = 3, 4
+    assert torch.equal(labels[:n], want) and int(labels[n]) == 77 and (kept == 1).all()
+    s.close()
+
+
+def test_two_samplers_beside_each_other():
+    """Two threads, a stream and a sampler each, the same rows: both draw what one draws alone."""
+    import threading
+    import torch
+    n, N = 300, 7_000
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    x, u = torch.randn((n, N), generator=g, device=DEV) * 3, torch.rand(n, generator=g, device=DEV)
+    p = torch.full((n,), 0.9, device=DEV)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.zeros((20, n), dtype=torch.int32, device=DEV) for _ in range(3)]
+    samplers = [B.cbd_sampler_create(n, N, hip_stream=st.cuda_stream) for st in [torch.cuda.current_stream()] + streams]
+    torch.cuda.synchronize()
+
+    def draw(i):
+        torch.cuda.set_device(0)
+        for j in range(20):
+            B.cbd_sampler_set_contexts(samplers[i], range(n), [[(c + j) % N, 5] for c in range(n)], [2.0] * n)
+            B.cbd_sample_labels(samplers[i], n, x.data_ptr(), N, 0, u.data_ptr(), outs[i][j].data_ptr(), top_p_ptr=p.data_ptr())
+
+    draw(0)
+    threads = [threading.Thread(target=draw, args=(i,)) for i in (1, 2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    for s in samplers:
+        B.cbd_sampler_free(s)
 
 
 def test_frequencies_follow_the_weights():

@@ -21,6 +21,7 @@ def test_layers_refuse_bad_descriptions():
     for kw in (dict(activation=6), dict(activation=-1), dict(weight_stride=7), dict(weight_stride=-8), dict(weight_stride=1 << 41),
                dict(bias_ptr=some + 2)):
         refused(B.cbd_layer_create, some, 8, 8, 0, **kw)
+    refused(B.cbd_layer_create, some, 65_536, 1_048_576, 0)   # (256 GB)
     refused(B.cbd_layer_apply, None, 1, 1, some, 8, 8, some, 8, 8)
     B.cbd_layer_free(None)
 
