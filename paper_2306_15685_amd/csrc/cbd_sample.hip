@@ -88,8 +88,10 @@ template <typename V> __device__ __forceinline__ V wave_scan(V v) {   // sum ove
   s += from_lanes<0x143, 0xc, 0xf>(s);
   return s;
 }
-__device__ __forceinline__ uint32_t last_lane(uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, 63); }
-__device__ __forceinline__ uint64_t last_lane(uint64_t v) { return (uint64_t)last_lane((uint32_t)(v >> 32)) << 32 | last_lane((uint32_t)v); }
+// (lane: the same in all lanes)
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane) { return (uint64_t)of_lane((uint32_t)(v >> 32), lane) << 32 | of_lane((uint32_t)v, lane); }
+template <typename V> __device__ __forceinline__ V last_lane(V v) { return of_lane(v, 63); }
 template <typename V> __device__ __forceinline__ V wave_sum(V v) { return last_lane(wave_scan(v)); }
 __device__ __forceinline__ uint32_t max32(uint32_t a, uint32_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint32_t min32(uint32_t a, uint32_t b) { return a < b ? a : b; }
@@ -475,7 +477,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     uint32_t rank = 0, place = 0;
     uint64_t w = 0, v = 0, upto = 0;
     if (have) {
-#pragma unroll 4
+#pragma unroll 16
       for (int j = 0; j < n; ++j) {
         const uint64_t other = near[j];
         rank += other > me;
@@ -635,12 +637,21 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     if (lane == 0) wave_c[wave] = above;
   }
   __syncthreads();
-  uint64_t total = 0, seen = 0;
-  for (int c = 0; c < kWaves * cells; ++c) {
-    total += cell_mass[c];
-    seen += cell_ties[c];
+  // (every wave by itself: lane l has cells l * kCells ..; one after the other they would take 256 reads' latency)
+  constexpr int kCells = (kWaves * kMaxCells + 63) / 64;
+  uint64_t lane_mass = 0, of_cell[kCells];
+  uint32_t lane_ties = 0, ties_of_cell[kCells];
+#pragma unroll
+  for (int i = 0; i < kCells; ++i) {
+    const int c = lane * kCells + i;
+    of_cell[i] = c < kWaves * cells ? cell_mass[c] : 0;
+    ties_of_cell[i] = c < kWaves * cells ? cell_ties[c] : 0;
+    lane_mass += of_cell[i];
+    lane_ties += ties_of_cell[i];
   }
-  const uint64_t kept_ties = seen < ties ? seen : (uint64_t)ties;
+  const uint32_t ties_upto = wave_scan(lane_ties);
+  uint64_t total = wave_sum(lane_mass);
+  const uint64_t seen = last_lane(ties_upto), kept_ties = seen < ties ? seen : (uint64_t)ties;
   total += kept_ties * w_cut;
   uint32_t kept = (uint32_t)kept_ties;
 #pragma unroll
@@ -661,18 +672,26 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   uint64_t target = (uint64_t)((double)random * (double)total);
   if (random >= 1.0f || target >= total) target = total - 1;
   // the cell in which the running sum passes the target; its wave goes through its turns
-  uint64_t run = 0;
-  uint32_t rank = 0;   // ties before
   auto kept_of = [&](uint32_t before, uint32_t n) {   // kept ones of n ties with `before` ahead of them
     return before >= ties ? 0u : min32(n, ties - before);
   };
-  int cell = 0;
-  for (;; ++cell) {
-    const uint64_t m = cell_mass[cell] + (uint64_t)kept_of(rank, cell_ties[cell]) * w_cut;
-    if (run + m > target) break;
-    run += m;
-    rank += cell_ties[cell];
+  uint32_t rank = ties_upto - lane_ties;   // ties before
+  const uint64_t lane_kept = lane_mass + (uint64_t)kept_of(rank, lane_ties) * w_cut, lane_upto = wave_scan(lane_kept);
+  const int at_lane = __ffsll((unsigned long long)__ballot(lane_upto > target)) - 1;
+  uint64_t run = lane_upto - lane_kept;
+  int cell = lane * kCells;
+#pragma unroll
+  for (int i = 0; i < kCells - 1; ++i) {
+    const uint64_t m = of_cell[i] + (uint64_t)kept_of(rank, ties_of_cell[i]) * w_cut;
+    if (cell == lane * kCells + i && run + m <= target) {
+      run += m;
+      rank += ties_of_cell[i];
+      ++cell;
+    }
   }
+  run = of_lane(run, at_lane);
+  rank = of_lane(rank, at_lane);
+  cell = (int)of_lane((uint32_t)cell, at_lane);
   if (wave != cell / cells) return;
   const int t0 = cell % cells * cell_turns, t1 = min(t0 + cell_turns, turns);
   bool found = false;

@@ -332,6 +332,7 @@ def test_refusals():
            dict(residual_ptr=o.data_ptr() + 2), dict(residual_ptr=o.data_ptr(), residual_channel_stride=32, residual_frame_stride=0),
            dict(residual_ptr=x.data_ptr(), residual_scale=INF), dict(residual_ptr=x.data_ptr(), residual_frame_stride=-1),
            dict(output_ptr=x.data_ptr()), dict(n_channels=65536, n_frames=65536, output_channel_stride=1 << 30),
+           dict(n_channels=1 << 15, n_frames=1 << 14, output_channel_stride=1 << 18),
            dict(input_channel_stride=1 << 61), dict(output_channel_stride=8, output_frame_stride=9)]
     for kw in bad:
         with pytest.raises(B.CbdError) as e:
