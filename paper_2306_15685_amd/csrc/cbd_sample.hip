@@ -300,6 +300,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   if constexpr (!kHeld) each_turn([&](int, const float (&x)[kVec]) __attribute__((always_inline)) {
     for (int j = 0; j < kVec; ++j) best = fmaxf(best, x[j]);
   });
+  const float thread_best = best;
   uint32_t best_key, unused;
   block_range(score_key(best), 0, &best_key, &unused);
   best = key_score(best_key);
@@ -330,7 +331,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   // the sum passes `want` becomes the interval.
   auto narrow = [&](auto by_mass, auto each, Interval &v, uint32_t end, auto want_of) __attribute__((always_inline)) {
     constexpr bool kMass = decltype(by_mass)::value;
-    const int width = 32 - __clz((int)((v.hi - max32(end, v.lo)) | 1u)), log2 = kBlock == 1024 ? 10 : 8;
+    const int width = 32 - __clz((int)((v.hi - max32(end, v.lo)) | 1u)), log2 = kBlock == 1024 ? 10 : kBlock == 512 ? 9 : 8;
     const int shift = width > log2 ? width - log2 : 0;
     __syncthreads();
     bins[tid] = 0;
@@ -372,6 +373,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     if (pick_bin < kBlock - 1 && (v.hi - v.lo) >> shift) v.lo = v.hi - (1u << shift) + 1u;
   };
   auto as_before = [](uint64_t, double want) { return want; };
+  auto end_of = [&](double reach) __attribute__((always_inline)) { return score_key((float)fmax((double)fminf(best, kLargest) - reach, -(double)kLargest)); };
   // ... and down to the keys that occur in it
   auto tighten = [&](auto each, Interval &v) __attribute__((always_inline)) {
     uint32_t top = 0, low = 0xFFFFFFFFu;
@@ -437,8 +439,7 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   auto search = [&](auto by_mass, Interval &v, auto want_of, bool list_all, uint32_t *listed) __attribute__((always_inline)) {
     constexpr bool kMass = decltype(by_mass)::value;
     // bins reach down to weights of 2^-46 (or, for counts, to scores 40 below the best): beyond, the search begins anew
-    const double reach = kMass ? 32.0 * (double)temperature : 40.0;
-    uint32_t end = score_key((float)fmax((double)fminf(best, kLargest) - reach, -(double)kLargest));
+    uint32_t end = end_of(kMass ? 32.0 * (double)temperature : 40.0);
     *listed = 0;
     for (bool begun = false;; begun = true) {
       narrow(by_mass, each_score, v, end, [&](uint64_t all, double want) __attribute__((always_inline)) { return begun ? want : want_of(all); });
@@ -539,6 +540,19 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
   };
   const bool by_count = k > 0 && k < N, by_share = top_p < 1.0f;
   uint32_t listed_from = 0;   // not 0: collect()'s sums are of larger keys, and the rest of the kept labels is in `near`
+  if (by_count && k <= kList / 2 && N >= 4 * kBlock) {
+    // The best scores of the threads are scores of as many labels: what is below the k-th of them is not among the first
+    // k.  With labels in no order few others are above it (177 for k = 128 and 256 threads, on average), so that the list
+    // is there without bins over the row (with top_k 50: 64 x 20,000 12 against 15 us, 256 x 200,000 63 against 89).
+    Interval v{last_key, best_key, 0, 0.0, kAllTies};
+    uint64_t threads = 0;
+    narrow(std::false_type(), [&](auto f) __attribute__((always_inline)) { f(thread_best); }, v, end_of(40.0),
+           [&](uint64_t all, double) __attribute__((always_inline)) { threads = all; return (double)min((uint64_t)k, all); });
+    if (threads >= (uint64_t)k && collect(v.lo, best_key) && n_near <= (uint32_t)kList) {
+      finish_list((int)n_near, (uint32_t)k, by_share ? (double)max(top_p, 0.0f) : -1.0, __builtin_inf());
+      return;
+    }
+  }
   if (by_count) {
     Interval v{last_key, best_key, 0, 0.0, kAllTies};
     uint64_t valid = 0;   // (no more labels than top_k: nothing is cut)
@@ -599,9 +613,12 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     }
     if (!by_count && !by_share) {
       // few labels are left, as a rule
-      if (collect(cut, best_key) && n_near <= (uint32_t)kList) {
-        finish_list((int)n_near, kAllTies, -1.0, __builtin_inf());
-        return;
+      if (collect(cut, best_key)) {
+        if (n_near <= (uint32_t)kList) {
+          finish_list((int)n_near, kAllTies, -1.0, __builtin_inf());
+          return;
+        }
+        listed_from = best_key;   // (all of them are in `near`)
       }
     }
   }

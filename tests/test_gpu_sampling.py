@@ -299,6 +299,35 @@ def test_captured_call_replays_with_new_values():
     s.close()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("labels", [1_030, 4_099, 20_000, 40_003])
+def test_few_labels_wherever_they_are(labels, dtype):
+    """top_k and min_p on rows whose best labels lie behind one another, are equal, are few, or are infinite."""
+    import torch
+    rng = np.random.default_rng(labels)
+    N = labels
+    rows = [np.sort(rng.normal(0, 3, N)), np.sort(rng.normal(0, 3, N))[::-1], np.zeros(N), rng.normal(0, 3, N)]
+    for n in (1, 49, 50, 51, 127, 128, 129, 300):   # labels that are not masked, in one stretch and spread
+        near, spread = np.full(N, -INF), np.full(N, -INF)
+        near[500:500 + n] = rng.normal(0, 2, n)
+        spread[rng.choice(N, n, replace=False)] = rng.normal(0, 2, n)
+        rows += [near, spread]
+    for n in (40, 50, 300):   # equal best ones
+        x = rng.normal(0, 1, N)
+        x[rng.choice(N, n, replace=False)] = 9.0
+        rows.append(x)
+        rows.append(np.where(x == 9.0, INF, x))
+    x = torch.from_numpy(np.stack(rows).astype(np.float32)).to(DEV).to(T(dtype))
+    s = Sampler(len(rows), N)
+    for k in (1, 50, 128, 129):
+        u = rng.random(len(rows))
+        check_rows(s, x, u, dtype, top_k=[k] * len(rows))
+        check_rows(s, x, u, dtype, top_k=[k] * len(rows), top_p=[0.75] * len(rows), temperature=[2.0] * len(rows))
+    for m in (0.5, 1e-3, 1e-6):
+        check_rows(s, x, rng.random(len(rows)), dtype, min_p=[m] * len(rows))
+    s.close()
+
+
 @pytest.mark.parametrize("with_channels", [True, False])
 def test_more_rows_than_one_launch_takes(with_channels):
     """2^21 + 70 rows of five scores; row i's best label is i mod 5."""
