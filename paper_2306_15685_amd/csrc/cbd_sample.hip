@@ -167,12 +167,11 @@ template <typename T, int kVec> struct Row {
   __device__ __forceinline__ void values(const Piece &p, float (&x)[kVec]) const {
     struct All { T v[kVec]; };
     const All e = __builtin_bit_cast(All, p.scores);
-    if (bits) {
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) x[j] = (float)e.v[j] + (p.listed >> j & 1 ? offset : 0.0f);
-    } else {
+    for (int j = 0; j < kVec; ++j) x[j] = (float)e.v[j] + 0.0f;
+    if (__ballot((p.listed & ((1u << kVec) - 1u)) != 0)) {   // (few of a row's turns have any)
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) x[j] = (float)e.v[j] + 0.0f;
+      for (int j = 0; j < kVec; ++j) x[j] += p.listed >> j & 1 ? offset : 0.0f;
     }
 #pragma unroll
     for (int j = 0; j < kVec; ++j) x[j] = fmaxf(x[j], -__builtin_inff());
