@@ -187,10 +187,11 @@ template <typename T, int kVec> struct Row {
 // down, and the bin where it passes the border is the next interval, narrowed to the keys that occur in it, until one
 // key is left.  All sums are of integers, so their order does not matter.
 //
-// Measured: 2048 x 6000 fp32 with min_p 28 us (the copy of its 49 MB takes 10), 64 x 20000 bf16 with top_k 50 and top_p 19,
-// 512 x 5003 fp16 with top_p 21, 256 x 200,000 fp32 with top_p 228 (copy 42): there the row is read three times (largest
-// score; masses of the bins; sums of what is kept and the labels near the cut), and the last two take some 26 vector
-// instructions of four cycles per label for its weight, 81 million in all: 132 us of issue.  Rows in LDS are bound by the
+// Measured: 2048 x 6000 fp32 with min_p and lists 27 us (the copy of its 49 MB takes 10), 64 x 20000 bf16 with top_k 50 and
+// top_p 14, 512 x 5003 fp16 with top_p 21, 256 x 200,000 fp32 with top_p and lists 201, without lists 176 (copy 42): there the
+// row is read three times (largest score; masses of the bins; sums of what is kept and the labels near the cut), and the last
+// two take some 26 vector instructions of four cycles per label for its weight, 71 million in all: 115 us of issue on the
+// 1024 SIMDs.  Rows in LDS are bound by the
 // same instructions and by the barriers between steps.
 template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
   constexpr int kWaves = kBlock / 64, kVec = kHeld ? 16 / sizeof(T) : 4, kMaxCells = kHeld ? 1 : 16;
