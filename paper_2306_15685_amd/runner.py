@@ -101,7 +101,8 @@ def contexts_from_words(graph_handle, sequences: list):
 
 
 class Session:
-    """A decoder sized for a workload, bound to torch's current stream."""
+    """A decoder sized for a workload, bound to the stream that is torch's current one when it is made: all of its work is
+    enqueued there, whatever stream or thread step() is called from."""
 
     def __init__(self, inp: Inputs, hash_log2: Optional[int] = None, table_location: int = 0,
                  records_per_frame: int = 0, graph_handle=None, biased: bool = True, lds_token_cap: int = 0,
@@ -117,7 +118,7 @@ class Session:
         Inputs with hidden vectors: the scores of each chunk are made by the output layer (cbd_layer_apply) in a buffer
         of one chunk, in front of cbd_advance on the same stream.  draw: a label per channel and frame is drawn from
         them as well, with the labels of the channel's listed arcs boosted; self.drawn has them (int32) and their
-        log-probabilities per segment, as device tensors [C, frames]."""
+        log-probabilities per segment, as device tensors [C, frames], written on the session's stream."""
         import torch
         self.torch = torch
         self.inp = inp
@@ -208,8 +209,11 @@ class Session:
                             self.random[s][t0 // w.chunk].data_ptr(), self.row_labels.data_ptr(),
                             channels_ptr=self.row_channels[n].data_ptr(), logprobs_ptr=self.row_logprobs.data_ptr(),
                             **{k + "_ptr": v.data_ptr() for k, v in self.settings.items()})
-        for out, of_rows in zip(self.drawn[s], (self.row_labels, self.row_logprobs)):
-            out[:, t0:t0 + n].copy_(of_rows[:rows].view(w.channels, n))
+        # (torch copies on its current stream, which need not be the session's: step() may run under another, or in a thread
+        # that has its own; the next chunk's labels go to the same rows)
+        with self.torch.cuda.stream(self.stream):
+            for out, of_rows in zip(self.drawn[s], (self.row_labels, self.row_logprobs)):
+                out[:, t0:t0 + n].copy_(of_rows[:rows].view(w.channels, n))
 
     def close(self):
         if self.layer is not None:
