@@ -593,10 +593,12 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     uint64_t yes = __ballot(from + lane <= best_key && enough(key_score(min32(from + lane, best_key)), least));
     if (from + 63u >= best_key) yes |= 1ull << (best_key - from);   // (the best always is)
     if (!yes || (yes & 1ull && from > last_key)) {
-      // not there: the whole interval, a 64th of what is left at a time; lo stays a key that is not enough or last_key
+      // not there (many scores to which the test gives the same result): the whole interval, a 64th of what is left at a
+      // time; lo stays a key that is not enough or last_key
       uint32_t lo = last_key, hi = best_key;   // hi is enough
       while (hi > lo) {
-        const uint32_t step = (hi - lo) / 64u + 1u, key = lo + (uint64_t)lane * step < hi ? lo + (uint32_t)lane * step : hi;
+        // (64 steps pass hi, but 63 need not: the last lane always has hi, so that one of them is enough)
+        const uint32_t step = (hi - lo) / 64u + 1u, key = lane < 63 && lo + (uint64_t)lane * step < hi ? lo + (uint32_t)lane * step : hi;
         const uint64_t ok = __ballot(key == hi || enough(key_score(key), least));
         const int l = __ffsll((unsigned long long)ok) - 1;
         const uint32_t at = __shfl(key, l), under = l > 0 ? __shfl(key, l - 1) + 1u : at;
