@@ -44,6 +44,7 @@ __device__ __forceinline__ uint32_t score_key(float x) {
 }
 __device__ __forceinline__ float key_score(uint32_t k) { return __uint_as_float(k ^ (~(uint32_t)((int32_t)k >> 31) | 0x80000000u)); }
 constexpr uint32_t kLowestKey = 0x00800000u;   // of the smallest finite score
+constexpr uint32_t kZeroKey = 0x80000000u;     // of 0
 
 // Weights as integers: exp((x - best) / temperature) in units of 2^-unit_bits, with relative error below 2^-36.
 struct Weigher {
@@ -371,6 +372,9 @@ template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBloc
     v.from_lo = pick_count;
     v.hi -= pick_bin << shift;
     if (pick_bin < kBlock - 1 && (v.hi - v.lo) >> shift) v.lo = v.hi - (1u << shift) + 1u;
+    // -0, which no score is, must not be the upper end: as a number it is not below the zeros, whose key is above it.  (The
+    // interval has a score, so that lo is below it.)
+    if (v.hi == kZeroKey - 1u) v.hi -= 1u;
   };
   auto as_before = [](uint64_t, double want) { return want; };
   auto end_of = [&](double reach) __attribute__((always_inline)) { return score_key((float)fmax((double)fminf(best, kLargest) - reach, -(double)kLargest)); };

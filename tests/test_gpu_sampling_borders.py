@@ -36,3 +36,37 @@ def test_min_p_of_one_at_high_temperatures(best, temperature, near, far, labels)
     for kw in (dict(), dict(top_p=[0.999] * 4), dict(top_k=[labels - 1] * 4), dict(top_k=[labels // 2 + 30] * 4, top_p=[0.9999] * 4)):
         S.check_rows(s, x, rng.random(4), "f32", temperature=t, min_p=one, **kw)
     s.close()
+
+
+@pytest.mark.parametrize("labels", [401, 3_000, 7_000, 20_000, 60_000])
+def test_cuts_among_zeros(labels):
+    """A best score just below a power of two, so that the borders between intervals of keys lie between the zeros and the
+    largest negative scores; half of the labels zero, the others negative and next to zero."""
+    import torch
+    rng = np.random.default_rng(labels)
+    rows, zeros = [], labels // 2
+    for best in (1.9999999, 0.99999994, 3.9999998, 2.0 ** -100 * (2 - 2.0 ** -23), 1.9999999):
+        x = -rng.uniform(5e-40, 2e-39, labels)
+        x[rng.permutation(labels)[:zeros]] = 0.0
+        x[rng.integers(0, labels)] = best
+        rows.append(x)
+    rows[3][rng.integers(0, labels, 20)] = -0.0
+    rows[4][rows[4] < 0] *= 1e36   # (further away)
+    x = torch.from_numpy(np.stack(rows).astype(np.float32)).to(DEV)
+    s = S.Sampler(5, labels)
+    for p in (0.3, 0.5, 0.75, 0.95):
+        S.check_rows(s, x, rng.random(5), "f32", top_p=[p] * 5)
+    for k in (2, 100, 150, 300, zeros // 2, zeros + 30):
+        S.check_rows(s, x, rng.random(5), "f32", top_k=[k] * 5)
+        S.check_rows(s, x, rng.random(5), "f32", top_k=[k] * 5, top_p=[0.75] * 5, min_p=[0.01] * 5)
+    # 16-bit scores reach such a best score by their offset
+    y = torch.zeros((2, labels), device=DEV)
+    y[:, labels // 2:] = -1e-39
+    y[0, labels - 3] = 1.0
+    y[1, 5] = 3.0
+    y = y.to(torch.bfloat16)
+    lists, offsets = [[labels - 3], [5]], np.array([0.9999999, 0.9999998], np.float32)
+    s.lists([0, 1], lists, offsets)
+    for p in (0.3, 0.75):
+        S.check_rows(s, y, rng.random(2), "bf16", lists, offsets, top_p=[p] * 2)
+    s.close()
