@@ -451,8 +451,8 @@ typedef struct cbd_layer_io {
 /*
  * Enqueues one application on `hip_stream` (of the layer's device).  Uses no memory besides the arguments', so calls on
  * several streams or from several threads may overlap, and a captured call may be replayed anywhere.  Results do not
- * depend on how often or beside what else the call runs.  Inputs and weights that are not finite give results that are
- * not finite in the rows and columns concerned.
+ * depend on how often or beside what else the call runs.  Inputs and weights that are not finite reach the results of their
+ * rows and columns only, as the formula has them (an infinity through relu or sigmoid may well be finite).
  */
 int32_t cbd_layer_apply(const cbd_layer *l, const cbd_layer_io *io, void *hip_stream);
 

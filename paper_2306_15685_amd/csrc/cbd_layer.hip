@@ -477,8 +477,8 @@ template <typename T, int FM, int FN, int kAhead> __global__ __launch_bounds__(6
       for (int a = 0; a < kAhead; ++a) {
         const int s = min(s0 + a, p.w_steps - 1);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) wv[a][j] = w[j][(int64_t)s * 64];
-        // (a step beyond the last counts as one beyond K: zeros)
+        for (int j = 0; j < FN; ++j) wv[a][j] = s0 + a < p.w_steps ? w[j][(int64_t)s * 64] : uint4v{0u, 0u, 0u, 0u};
+        // (a step beyond the last counts as one beyond K: zeros on both sides, as zero times an infinite weight is NaN)
         const int k = (s0 + a) * kStep;
 #pragma unroll
         for (int i = 0; i < FM; ++i) xv[a][i] = load_piece<T>(src[i], k, p.K - (lane >> 4) * kElems);
