@@ -529,10 +529,12 @@ namespace {
 
 using cbd::LayerParams;
 
-// calls f(O(), std::bool_constant<activation>()) for the output's type and whether there is an activation
+// calls f(O(), std::bool_constant<activation>()) for the output's type and whether there is an activation (or a scale above
+// 1: without an activation whole tiles scale sum and bias before they add them, and a scaled bias could leave fp32's range
+// where the scaled result does not)
 template <typename F> void with_output(const LayerParams &p, F f) {
   auto with_type = [&](auto o) {
-    if (p.act == CBD_ACT_NONE) f(o, std::false_type());
+    if (p.act == CBD_ACT_NONE && std::fabs(p.scale) <= 1.0f) f(o, std::false_type());
     else f(o, std::true_type());
   };
   if (p.out_dtype == CBD_F32) with_type(0.0f);

@@ -30,3 +30,22 @@ def test_an_infinite_weight_gives_infinities(dtype, rows, K, N):
         want[:, 0] = x[0, :, at].float() * -INF
         assert torch.equal(got, want), at
         layer.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,K,N", [(5, 40, 24), (128, 64, 128), (1024, 64, 2048), (2560, 32, 3328), (4096, 576, 4352)])
+def test_sums_that_only_a_scale_takes_out_of_range(dtype, rows, K, N):
+    """scale * (sum + bias): the sum's and the bias's own multiples are beyond fp32, the result is not."""
+    import torch
+    g = L.gen(K)
+    top = 2.0 ** 127
+    x, w = torch.zeros((1, rows, K), device=DEV, dtype=L.T(dtype)), torch.zeros((N, K), device=DEV, dtype=L.T(dtype))
+    small = L.whole((rows,), "f32", g)
+    x[0, :, 0] = small.to(L.T(dtype)) / 8 + 1
+    w[:, 0] = top
+    bias = torch.full((N,), -top, device=DEV)
+    layer = L.Layer(w, bias, dtype)
+    for scale in (2.0, -2.0, 1.5, 1.0, 0.25):
+        got = layer.apply(x, torch.zeros((1, rows, N), device=DEV), scale)
+        assert torch.equal(got[0], (small / 8 * scale)[:, None].mul(top).expand(rows, N)), scale
+    layer.close()
