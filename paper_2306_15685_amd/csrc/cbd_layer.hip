@@ -331,7 +331,7 @@ template <typename T> __global__ __launch_bounds__(256) void pack_weight_kernel(
 // silu 113 us (880 and 950 TFLOP/s; the matrix units are busy half of the cycles: the stores of a tile's results and its
 // first loads are not covered by products), fp32 1600 x 512 -> 3000 49.5 us (99 TFLOP/s, busy 73 %: the last of 1200 tiles).
 template <typename T, typename O, bool kActivation, int WM, int WN, int FM, int FN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LayerParams p, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LayerParams p, int first_m, int tiles_m, int tiles_n) {
   constexpr int kThreads = 64 * WM * WN, BM = WM * FM * 16, kElems = 16 / sizeof(T), kTileK = 8 * kElems;
   constexpr int kPieces = BM * 8 / kThreads;   // 16-byte pieces of a K tile per thread
   __shared__ uint4v lds[2][BM * 8];
@@ -339,6 +339,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LayerParams p, in
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   int tile_m, tile_n;
   place_tile(blockIdx.x, tiles_m, tiles_n, &tile_m, &tile_n);
+  tile_m += first_m;   // (the launch's first row of tiles)
   place_rows(p, tile_m * BM, BM, rows_at);
   // this thread's pieces of the input: rows tid / 8 + i * (threads / 8), piece tid % 8 of each K tile
   const T *src[kPieces];
@@ -544,12 +545,17 @@ template <typename F> void with_output(const LayerParams &p, F f) {
 
 template <typename T, int WM, int WN, int FM, int FN> hipError_t launch_tiles(const LayerParams &p, hipStream_t st) {
   const int tiles_m = (p.rows + WM * FM * 16 - 1) / (WM * FM * 16), tiles_n = (p.N + WN * FN * 16 - 1) / (WN * FN * 16);
-  if ((int64_t)tiles_m * tiles_n * (64 * WM * WN) > 0xFFFFFFFFll) return hipErrorInvalidConfiguration;   // (threads of a launch; up to 128 outputs never)
-  with_output(p, [&](auto o, auto act) {
-    hipLaunchKernelGGL((cbd::tile_kernel<T, decltype(o), decltype(act)::value, WM, WN, FM, FN>), dim3((unsigned)tiles_m * (unsigned)tiles_n),
-                       dim3(64 * WM * WN), 0, st, p, tiles_m, tiles_n);
-  });
-  return hipGetLastError();
+  const int most = (int)(0xFFFFFFFFll / (64 * WM * WN) / tiles_n);   // rows of tiles in a launch, which has fewer than 2^32 threads
+  for (int first = 0; first < tiles_m; first += most) {
+    const int n = std::min(most, tiles_m - first);
+    with_output(p, [&](auto o, auto act) {
+      hipLaunchKernelGGL((cbd::tile_kernel<T, decltype(o), decltype(act)::value, WM, WN, FM, FN>), dim3((unsigned)n * (unsigned)tiles_n),
+                         dim3(64 * WM * WN), 0, st, p, first, n, tiles_n);
+    });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T, int FM, int FN, int kAhead> hipError_t launch_narrow(const LayerParams &p, hipStream_t st) {

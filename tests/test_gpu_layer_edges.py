@@ -49,3 +49,24 @@ def test_sums_that_only_a_scale_takes_out_of_range(dtype, rows, K, N):
         got = layer.apply(x, torch.zeros((1, rows, N), device=DEV), scale)
         assert torch.equal(got[0], (small / 8 * scale)[:, None].mul(top).expand(rows, N)), scale
     layer.close()
+
+
+def test_more_tiles_than_one_launch_takes():
+    """2^28 rows of 129 outputs: two launches of tiles, a few rows in the second.  Row r's input is r mod 32."""
+    import torch
+    rows, N = 2 ** 28 + 100, 129
+    if torch.cuda.mem_get_info()[0] < 100 * 2 ** 30:
+        pytest.skip("needs 100 GB of free device memory")
+    x = (torch.arange(rows, device=DEV, dtype=torch.int32) % 32).float()
+    w = (torch.arange(N, device=DEV) % 5 - 2).float()[:, None].contiguous()
+    out = torch.full((rows + 1, N), 7.0, device=DEV, dtype=torch.bfloat16)
+    layer = L.Layer(w, None, "f32")
+    layer.apply(x.view(1, rows, 1), out[:rows].view(1, rows, N))
+    want = (torch.arange(32, device=DEV).float()[:, None] * w[:, 0]).to(torch.bfloat16).repeat(2 ** 15, 1)   # of 2^20 rows
+    for at in range(0, rows, 2 ** 20):
+        n = min(2 ** 20, rows - at)
+        assert torch.equal(out[at:at + n], want[:n]), at
+    assert (out[rows] == 7.0).all()
+    layer.close()
+    del x, out, want
+    torch.cuda.empty_cache()
