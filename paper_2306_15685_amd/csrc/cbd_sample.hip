@@ -886,8 +886,9 @@ int32_t cbd_sampler_set_contexts(cbd_sampler *s, const int32_t *channels, int32_
   if (cbd::is_capturing(s->stream)) return fail(CBD_E_INVALID, "sampler_set_contexts: the stream is being captured");
   cbd::DeviceScope on(s->device);
   HIPCHK(on.error);
-  for (int32_t i0 = 0; i0 < n_channels; i0 += kUpload) {
-    const int32_t m = std::min(kUpload, n_channels - i0);
+  // (64 bits: the start of the piece behind the last one may be beyond 32)
+  for (int64_t i0 = 0; i0 < n_channels; i0 += kUpload) {
+    const int32_t m = (int32_t)std::min<int64_t>(kUpload, n_channels - i0);
     int slot = 0;
     HIPCHK(s->ring.acquire(&slot));
     memcpy(s->ring.host[slot], channels + i0, sizeof(int32_t) * (size_t)m);
@@ -900,8 +901,8 @@ int32_t cbd_sampler_set_contexts(cbd_sampler *s, const int32_t *channels, int32_
     HIPCHK(s->ring.release(slot, s->stream));
   }
   int32_t channel = 0;   // position whose list entry k belongs to
-  for (int32_t k0 = 0; k0 < total; k0 += kUpload) {
-    const int32_t m = std::min(kUpload, total - k0);
+  for (int64_t k0 = 0; k0 < total; k0 += kUpload) {
+    const int32_t m = (int32_t)std::min<int64_t>(kUpload, total - k0);
     int slot = 0;
     HIPCHK(s->ring.acquire(&slot));
     int2 *h = (int2 *)s->ring.host[slot];

@@ -70,3 +70,19 @@ def test_cuts_among_zeros(labels):
     for p in (0.3, 0.75):
         S.check_rows(s, y, rng.random(2), "bf16", lists, offsets, top_p=[p] * 2)
     s.close()
+
+
+def test_as_many_list_entries_as_there_may_be():
+    """2^31 - 1 entries, all but the last three label 0 of channel 1."""
+    import torch
+    from paper_2306_15685_amd import binding as B
+    total, N = 2 ** 31 - 1, 40
+    labels = np.zeros(total, np.int32)   # (pages that are only read take no memory)
+    labels[-3:] = 5, 39, 7
+    s = S.Sampler(3, N)
+    print("setting the lists", flush=True)
+    B.cbd_sampler_set_contexts(s.h, [1, 2], None, [2.0, 3.0], packed=(labels, np.array([0, total - 1, total], np.int32)))
+    x = torch.from_numpy(np.random.default_rng(1).normal(0, 1, (3, N)).astype(np.float32)).to(DEV)
+    for u in (0.05, 0.4, 0.9):
+        S.check_rows(s, x, [u] * 3, "f32", [[], [0, 5, 39], [7]], [0.0, 2.0, 3.0], top_k=[4] * 3)
+    s.close()
