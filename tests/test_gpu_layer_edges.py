@@ -3,6 +3,7 @@ own size, more tiles than a launch takes."""
 import numpy as np
 import pytest
 
+import score_reference as R
 import test_gpu_layers as L
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +71,27 @@ def test_more_tiles_than_one_launch_takes():
     layer.close()
     del x, out, want
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,N", [(200, 40), (2048, 256)])
+@pytest.mark.parametrize("act,steps", [("tanh", lambda y: 8 + 0 * y), ("gelu", lambda y: 20 + 0 * y),
+                                       ("sigmoid", lambda y: 1.25 * y + 6), ("silu", lambda y: 1.25 * y + 6)])
+def test_activations_relative_to_their_own_size(act, steps, rows, N):
+    """One product, rounded as fp32 does: the activation itself, in fp32, over -12 .. 12 and at small |y|.  Half
+    steps, largest first: tanh, the exponential's part at |y| = 0.6 is 0.86 of (1.5 for its argument + 2 + 1 + 2 for the quotient)
+    and 1 for the sum.  gelu, 8 for t (3, of which g takes up to 2.7 times), 4 for the polynomial, 2 for its fit, 3 for the
+    exponential, 1 for each of three products.  sigmoid, silu: 1.25 |y| + 2 for the exponential, 1 for the sum, 2 for the
+    reciprocal, 1 for the product."""
+    import torch
+    g = L.gen(5)
+    x = torch.rand((1, rows, 1), generator=g, device=DEV) * 2 - 1
+    w = 2.0 ** torch.randint(-30, 4, (N, 1), generator=g, device=DEV).float() * torch.where(torch.rand((N, 1), generator=g, device=DEV) < 0.5, 1.5, 1.0)
+    w[: N // 2] = torch.rand((N // 2, 1), generator=g, device=DEV) * 12
+    y = (x[0] * w[:, 0]).double()   # (fp32 products, as the layer makes them)
+    layer = L.Layer(w, None, "f32", act)
+    got = layer.apply(x, torch.zeros((1, rows, N), device=DEV))[0].double()
+    want = R.act64(act, y)
+    error = (got - want).abs() / want.abs() * 2.0 ** 24   # (in half steps)
+    print(act, "largest error in half steps", float(error.max()), flush=True)
+    assert (want != 0).all() and (error <= steps(y.abs())).all()
+    layer.close()
