@@ -1,6 +1,7 @@
 """Builds the HIP library in-tree for gfx950 (hipcc cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import functools
 import os
 import subprocess
 import sys
@@ -65,17 +66,22 @@ def build(force: bool = True, verbose: bool = False, profile: bool = False, spre
     return lib
 
 
+@functools.lru_cache(maxsize=None)   # (it takes a minute)
 def resource_usage() -> dict:
-    """Compiles the device code once more with the compiler's resource remarks on and returns, per kernel,
+    """Compiles the device code of all units once more with the compiler's resource remarks on and returns, per kernel,
     {"vgprs", "vgpr_spill", "scratch", "lds"} (name = demangled-ish substring of the kernel symbol)."""
     import re
     import tempfile
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     flags = [f for f in HIPCC_FLAGS if f not in ("-Wall", "-Wno-unused-result")]
     with tempfile.TemporaryDirectory() as tmp:
-        cmd = [hipcc, *flags, "--cuda-device-only", "-c", "-Rpass-analysis=kernel-resource-usage",
-               "-o", os.path.join(tmp, "dev.o"), SRC]
-        out = subprocess.run(cmd, check=True, capture_output=True, text=True).stderr
+        def remarks(src: str) -> str:
+            cmd = [hipcc, *flags, "--cuda-device-only", "-c", "-Rpass-analysis=kernel-resource-usage",
+                   "-o", os.path.join(tmp, os.path.basename(src) + ".o"), src]
+            return subprocess.run(cmd, check=True, capture_output=True, text=True).stderr
+
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            out = "".join(pool.map(remarks, SOURCES))
     usage, cur = {}, None
     for line in out.splitlines():
         m = re.search(r"remark: Function Name: (\S+)", line)
