@@ -86,3 +86,25 @@ def test_as_many_list_entries_as_there_may_be():
     for u in (0.05, 0.4, 0.9):
         S.check_rows(s, x, [u] * 3, "f32", [[], [0, 5, 39], [7]], [0.0, 2.0, 3.0], top_k=[4] * 3)
     s.close()
+
+
+@pytest.mark.parametrize("labels,dtype", [(1_048_575, "bf16"), (1_048_576, "f32")])
+def test_as_many_labels_as_there_may_be(labels, dtype):
+    """Scores as they come, all equal (the largest sum of weights there is, cuts among the ties), and few distinct ones; random
+    numbers at both ends."""
+    import torch
+    rng = np.random.default_rng(labels)
+    rows = rng.normal(0, 2, (4, labels)).astype(np.float32)
+    rows[1] = 3.0
+    rows[2] = rng.integers(0, 3, labels)
+    rows[3, 1:] = -np.inf
+    rows[3, labels - 1] = rows[3, 0]
+    x = torch.from_numpy(rows).to(DEV).to(S.T(dtype))
+    s = S.Sampler(4, labels)
+    for u in (0.0, 0.37, 0.9999999, 1.0):
+        S.check_rows(s, x, [u] * 4, dtype)
+        S.check_rows(s, x, [u] * 4, dtype, top_p=[0.3, 0.71, 0.6, 0.4])
+    S.check_rows(s, x, rng.random(4), dtype, top_k=[100, 70_001, 800_000, 1])
+    S.check_rows(s, x, rng.random(4), dtype, top_k=[900_000, 1_000_003, 500, 2], top_p=[0.9, 0.31, 0.95, 0.7], temperature=[0.7, 1.3, 2.0, 1.0])
+    S.check_rows(s, x, rng.random(4), dtype, min_p=[0.05, 0.5, 0.3, 1.0])
+    s.close()
