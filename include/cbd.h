@@ -440,12 +440,12 @@ typedef struct cbd_layer_io {
   int64_t input_channel_stride; /* >= 0; rows may overlap (a context of frames spliced into one row) */
   int64_t input_frame_stride;
   void *output;                 /* DEVICE; its rows must overlap neither each other nor the input */
-  int64_t output_channel_stride;
-  int64_t output_frame_stride;
+  int64_t output_channel_stride; /* whole channels behind one another (>= (n_frames - 1) * frame stride + out_features), */
+  int64_t output_frame_stride;   /* or whole frames */
   int32_t output_dtype;         /* cbd_dtype of output and residual */
   float scale;                  /* finite */
-  const void *residual;         /* DEVICE, or NULL = none; may be the output itself (same address and strides) */
-  int64_t residual_channel_stride; /* >= 0 */
+  const void *residual;         /* DEVICE, or NULL = none; the output itself (same address and strides) or apart from it */
+  int64_t residual_channel_stride; /* >= 0; rows may be the same */
   int64_t residual_frame_stride;
   float residual_scale;         /* finite */
 } cbd_layer_io;
@@ -453,7 +453,9 @@ typedef struct cbd_layer_io {
 /*
  * Enqueues one application on `hip_stream` (of the layer's device).  Uses no memory besides the arguments', so calls on
  * several streams or from several threads may overlap, and a captured call may be replayed anywhere.  Results do not
- * depend on how often or beside what else the call runs.  Inputs and weights that are not finite reach the results of their
+ * depend on how often or beside what else the call runs.  They do depend, in their last bits, on the call's size: how many
+ * rows there are decides how the sums along K are split, and the same row among more, fewer or other rows may differ by the
+ * rounding of fp32 sums.  Scores that have to be equal bit for bit need calls of equal sizes.  Inputs and weights that are not finite reach the results of their
  * rows and columns only, as the formula has them (an infinity through relu or sigmoid may well be finite).
  */
 int32_t cbd_layer_apply(const cbd_layer *l, const cbd_layer_io *io, void *hip_stream);
@@ -472,10 +474,11 @@ int32_t cbd_layer_apply(const cbd_layer *l, const cbd_layer_io *io, void *hip_st
  *          least; >= 1 (or NaN) = all
  *   min_p: labels with w_i < min(min_p, 1) are dropped; <= 0 (or NaN) = none
  *   label: the lowest one at which the running sum, by label, of the kept weights exceeds random * their total
- * Weights are summed as 64-bit integers in units of 2^-min(50, 62 - ceil(log2 num_labels)).  If scores of +inf occur, their
- * labels share the mass equally.
+ * Weights are summed as 64-bit integers in units of 2^-min(50, 62 - ceil(log2 num_labels)), and one below half a unit counts as
+ * nothing; only where random is 0 the label is the lowest kept one whose weight is above 0 in 64-bit floating point.  If scores
+ * of +inf occur, their labels share the mass equally.
  */
-typedef struct cbd_sampler cbd_sampler; /* opaque; owns the channels' lists */
+typedef struct cbd_sampler cbd_sampler; /* opaque; owns the channels' lists; one host thread at a time */
 
 /* For up to num_channels lists (>= 1) over rows of num_labels scores (1 .. 1048576), on the current HIP device; all work
  * is enqueued on `hip_stream` (a hipStream_t of that device, NULL = the null stream). */
@@ -512,7 +515,8 @@ typedef struct cbd_sample_desc {
 
 /*
  * Enqueues one draw per row.  Everything is read when the stream reaches the call (a captured call may be replayed with
- * new values in the same arrays); no memory besides the arguments' and the lists is used.
+ * new values in the same arrays); no memory besides the arguments' and the lists is used.  A replay on another stream than
+ * the sampler's has to be ordered behind cbd_sampler_set_contexts by the caller.
  */
 int32_t cbd_sample_labels(cbd_sampler *s, const cbd_sample_desc *desc);
 

@@ -85,7 +85,8 @@ __device__ __forceinline__ float activate(int act, float y) {
     case CBD_ACT_GELU: {
       // y Phi(y).  The tail Phi(-m), m = |y|, is exp(-m^2 / 2) g(m), and g falls from 1/2 like 1 / m: it is t = 1 / (1 + 0.3 m)
       // times a polynomial in t, fitted to a relative 1.2e-7 for m up to 13 (the tail leaves fp32's range there).  What
-      // rounding takes from m^2 and from the exponent is put back in first order, or it would count some 50 times.
+      // rounding takes from m^2 and from the exponent is put back in first order, or it would count some 50 times.  (12800 x
+      // 1024 -> 4096 in bf16 128 us; with silu 110, with tanh 117.)
       const float m = fminf(fabsf(y), 16.0f), t = fast_rcp(fmaf(0.3f, m, 1.0f));
       float g = fmaf(0.0360896401f, t, -0.158936828f);
       g = fmaf(g, t, 0.209351301f);
@@ -207,8 +208,8 @@ template <typename O, bool kResidual> __device__ __forceinline__ void store_whol
 // lane holds, of row lane % 16 of each row block, eight neighbouring outputs per pair of blocks, and the four lanes of a
 // row 32: one 16-byte store (two for fp32) a lane fills 64 bytes of a row.
 //
-// A tile that lies within the rows and outputs: straight-line code for layers without activation (15 instructions for
-// eight outputs), a loop over the row blocks for the others.
+// A tile that lies within the rows and outputs: straight-line code for layers without activation and with a scale of at
+// most 1 (15 instructions for eight outputs), a loop over the row blocks for the others.
 template <typename O, bool kResidual, bool kActivation, int FM, int FN>
 __device__ __forceinline__ void finish_whole(const LayerParams &p, float4v (&acc)[FM][FN], const longlong2 *rows_at, int n, int lane) {
   float bias[FN / 2][8];

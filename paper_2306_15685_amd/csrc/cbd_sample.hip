@@ -192,8 +192,9 @@ template <typename T, int kVec> struct Row {
 // top_p 14, 512 x 5003 fp16 with top_p 21, 256 x 200,000 fp32 with top_p and lists 201, without lists 176 (copy 42): there the
 // row is read three times (largest score; masses of the bins; sums of what is kept and the labels near the cut), and the last
 // two take some 26 vector instructions of four cycles per label for its weight, 71 million in all: 115 us of issue on the
-// 1024 SIMDs.  Rows in LDS are bound by the
-// same instructions and by the barriers between steps.
+// 1024 SIMDs.  Rows in LDS spend less than half of their time issuing instructions (12 of 25 us with min_p, 9 of 22 with
+// top_p, by their counts); the rest is waiting: for the row's first read, a turn at a time, and at the barriers of some fifteen
+// steps.
 template <typename T, int kBlock, bool kHeld> __global__ __launch_bounds__(kBlock) void sample_kernel(SampleParams p) {
   constexpr int kWaves = kBlock / 64, kVec = kHeld ? 16 / sizeof(T) : 4, kMaxCells = kHeld ? 1 : 16;
   // (512 against 256 labels near the cut: 512 x 5003 in f16 with top_p 0.9 21 us against 28)
@@ -792,8 +793,8 @@ template <typename T, int kBlock, bool kHeld> void launch_rows(const cbd::Sample
 
 // Threads per row: for few labels a step costs as much as its barriers, and two or more workgroups on a compute unit hide
 // each other's; a row alone on its compute unit with some thousand labels is faster with more threads.  With top_p 0.9,
-// fp32, threads 256 / 512 / 1024: 512 x 1500 12.1 / 13.6 / 23.9 us, 1 x 1500 9.8 / 9.5 / 11.6, 1 x 6000 16.9 / 13.6 / 14.7,
-// 256 x 6000 18.0 / 15.2 / -, 512 x 5003 in f16 28 / 28 / 31.
+// fp32, threads 256 / 512 / 1024: 512 x 1500 12.2 / 12.8 / 24.4 us, 1 x 1500 10.1 / 9.4 / 11.8, 1 x 6000 14.6 / 12.4 / 14.1,
+// 256 x 6000 18.5 / 14.7 / 16.2, 512 x 6000 21.3 / 19.2 / 29.7, 512 x 5003 in f16 21.0 / 21.4 / 29.4.
 template <typename T> void launch_sample(const cbd::SampleParams &p, int n, hipStream_t st) {
   if (p.num_labels <= 2048 || (p.num_labels <= 8192 && n > 256)) launch_rows<T, 256, true>(p, n, st);
   else if (p.num_labels <= 8192) launch_rows<T, 512, true>(p, n, st);
