@@ -208,8 +208,8 @@ template <typename O, bool kResidual> __device__ __forceinline__ void store_whol
 // lane holds, of row lane % 16 of each row block, eight neighbouring outputs per pair of blocks, and the four lanes of a
 // row 32: one 16-byte store (two for fp32) a lane fills 64 bytes of a row.
 //
-// A tile that lies within the rows and outputs: straight-line code for layers without activation and with a scale of at
-// most 1 (15 instructions for eight outputs), a loop over the row blocks for the others.
+// A tile that lies within the rows and outputs: straight-line code for layers without activation, a loop over the row blocks
+// for the others.
 template <typename O, bool kResidual, bool kActivation, int FM, int FN>
 __device__ __forceinline__ void finish_whole(const LayerParams &p, float4v (&acc)[FM][FN], const longlong2 *rows_at, int n, int lane) {
   float bias[FN / 2][8];
@@ -217,15 +217,13 @@ __device__ __forceinline__ void finish_whole(const LayerParams &p, float4v (&acc
   for (int j = 0; j < FN / 2; ++j) load_bias(p, n + j * 32, bias[j]);
   if (!kActivation) {
 #pragma unroll
-    for (int j = 0; j < FN * 4; ++j) bias[j / 8][j % 8] *= p.scale;
-#pragma unroll
     for (int i = 0; i < FM; ++i) {
       const longlong2 at = rows_at[i * 16 + (lane & 15)];
 #pragma unroll
       for (int j = 0; j < FN / 2; ++j) {
         float8v v;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = fmaf(acc[i][2 * j + q / 4][q % 4], p.scale, bias[j][q]);
+        for (int q = 0; q < 8; ++q) v[q] = (acc[i][2 * j + q / 4][q % 4] + bias[j][q]) * p.scale;
         store_whole<O, kResidual>(p, at.x, at.y, n + j * 32, v);
       }
     }
@@ -547,12 +545,10 @@ namespace {
 
 using cbd::LayerParams;
 
-// calls f(O(), std::bool_constant<activation>()) for the output's type and whether there is an activation (or a scale above
-// 1: without an activation whole tiles scale sum and bias before they add them, and a scaled bias could leave fp32's range
-// where the scaled result does not)
+// calls f(O(), std::bool_constant<activation>()) for the output's type and whether there is an activation
 template <typename F> void with_output(const LayerParams &p, F f) {
   auto with_type = [&](auto o) {
-    if (p.act == CBD_ACT_NONE && std::fabs(p.scale) <= 1.0f) f(o, std::false_type());
+    if (p.act == CBD_ACT_NONE) f(o, std::false_type());
     else f(o, std::true_type());
   };
   if (p.out_dtype == CBD_F32) with_type(0.0f);
