@@ -86,7 +86,7 @@ __device__ __forceinline__ float activate(int act, float y) {
       // y Phi(y).  The tail Phi(-m), m = |y|, is exp(-m^2 / 2) g(m), and g falls from 1/2 like 1 / m: it is t = 1 / (1 + 0.3 m)
       // times a polynomial in t, fitted to a relative 1.2e-7 for m up to 13 (the tail leaves fp32's range there).  What
       // rounding takes from m^2 and from the exponent is put back in first order, or it would count some 50 times.  (12800 x
-      // 1024 -> 4096 in bf16 128 us; with silu 110, with tanh 117.)
+      // 1024 -> 4096 in bf16 129 us; with silu 107, with tanh 118.)
       const float m = fminf(fabsf(y), 16.0f), t = fast_rcp(fmaf(0.3f, m, 1.0f));
       float g = fmaf(0.0360896401f, t, -0.158936828f);
       g = fmaf(g, t, 0.209351301f);
@@ -208,37 +208,20 @@ template <typename O, bool kResidual> __device__ __forceinline__ void store_whol
 // lane holds, of row lane % 16 of each row block, eight neighbouring outputs per pair of blocks, and the four lanes of a
 // row 32: one 16-byte store (two for fp32) a lane fills 64 bytes of a row.
 //
-// A tile that lies within the rows and outputs: straight-line code for layers without activation, a loop over the row blocks
-// for the others.
+// A tile that lies within the rows and outputs: code for each row block.  A loop over them would be an eighth of it, but no
+// running index reaches registers, and what picks a block's sums in their place spilled a third of those of 128 x 256 tiles:
+// 12800 x 1024 -> 4096 with silu and residual 165 us, so 121.
 template <typename O, bool kResidual, bool kActivation, int FM, int FN>
 __device__ __forceinline__ void finish_whole(const LayerParams &p, float4v (&acc)[FM][FN], const longlong2 *rows_at, int n, int lane) {
   float bias[FN / 2][8];
 #pragma unroll
   for (int j = 0; j < FN / 2; ++j) load_bias(p, n + j * 32, bias[j]);
-  if (!kActivation) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const longlong2 at = rows_at[i * 16 + (lane & 15)];
-#pragma unroll
-      for (int j = 0; j < FN / 2; ++j) {
-        float8v v;
-#pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = (acc[i][2 * j + q / 4][q % 4] + bias[j][q]) * p.scale;
-        store_whole<O, kResidual>(p, at.x, at.y, n + j * 32, v);
-      }
-    }
-    return;
-  }
-#pragma unroll 1
   for (int i = 0; i < FM; ++i) {
     float v[FN * 4];
 #pragma unroll
-    for (int k = 0; k < FM; ++k)   // (register arrays take no running index)
-      if (k == i) {
-#pragma unroll
-        for (int j = 0; j < FN * 4; ++j) v[j] = acc[k][j / 4][j % 4] + bias[j / 8][j % 8];
-      }
-    activate_by(p.act, v);
+    for (int j = 0; j < FN * 4; ++j) v[j] = acc[i][j / 4][j % 4] + bias[j / 8][j % 8];
+    if (kActivation) activate_by(p.act, v);
     const longlong2 at = rows_at[i * 16 + (lane & 15)];
 #pragma unroll
     for (int j = 0; j < FN / 2; ++j) {
@@ -342,8 +325,8 @@ template <typename T> __global__ __launch_bounds__(256) void pack_weight_kernel(
 // Tiles.  A workgroup of WM x WN waves makes (WM * FM * 16) rows x (WN * FN * 16) outputs; a wave FM x FN blocks of 16 x
 // 16.  Input rows go through LDS, 128 bytes of K at a time, two buffers; weights come straight from the packed layout
 // into registers, one such step ahead: no two waves of a workgroup read the same weights, so LDS would only delay them,
-// and its bandwidth is left to the rows.  Measured (12800 rows): 1024 -> 6000 in bf16 to fp32 179 us, 1024 -> 4096 with
-// silu 113 us (880 and 950 TFLOP/s; the matrix units are busy half of the cycles: the stores of a tile's results and its
+// and its bandwidth is left to the rows.  Measured (12800 rows): 1024 -> 6000 in bf16 to fp32 177 us, 1024 -> 4096 with
+// silu 108 us (885 and 995 TFLOP/s; the matrix units are busy half of the cycles: the stores of a tile's results and its
 // first loads are not covered by products), fp32 1600 x 512 -> 3000 49.5 us (99 TFLOP/s, busy 73 %: the last of 1200 tiles).
 template <typename T, typename O, bool kActivation, int WM, int WN, int FM, int FN>
 __global__ __launch_bounds__(64 * WM * WN, 2) void tile_kernel(LayerParams p, int first_m, int tiles_m, int tiles_n) {

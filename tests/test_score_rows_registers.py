@@ -11,13 +11,13 @@ def usage():
 
 
 def test_tiles_keep_two_waves_on_a_simd(usage):
-    """At most 256 registers.  Tiles of 128 x 256 need all of them: what is spilled is of the epilogue (accumulators beside the
-    temporaries of an activation), a few hundred bytes once a tile; no other tile spills."""
+    """At most 256 registers.  Tiles of 128 x 256 need all of them and may spill a few numbers that are used once a tile; no
+    other tile spills."""
     tiles = {k: v for k, v in usage.items() if "tile_kernel" in k}
     assert len(tiles) == 2 * 3 * 2 * 4 + 3 * 2   # (16-bit types x output types x activation or not x four sizes; fp32: one size)
     for k, v in tiles.items():
         kind = re.search(r"Lb([01])ELi1ELi4ELi(\d)ELi(\d)E", k).groups()
-        limit = 0 if kind[1:] != ("8", "4") else 16 if kind[0] == "0" else 384
+        limit = 16 if kind[1:] == ("8", "4") else 0
         assert v["vgprs"] <= 256 and v["scratch"] <= limit, (k, v)
         if kind[1:] in (("2", "2"), ("4", "2")):
             assert v["vgprs"] <= 128, (k, v)   # (four waves)
